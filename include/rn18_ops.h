@@ -78,6 +78,74 @@ int rn18op_maxpool_bwd(int prec, const void* dy, const uint8_t* arg, void* dx, i
  * aligned device pointers. The oracle's rounding points assume this rule. */
 int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* hip_stream);
 
+/* ---- Row operators -------------------------------------------------------
+ * Layer norm, a teacher's top logits and the distillation loss work on R rows
+ * of a matrix whose rows are `ld` elements apart (ld >= the width; any ld and
+ * any width >= 1). Their tensors of the storage type need only the alignment
+ * of one element, their fp32 and int32 arrays that of 4 bytes; rows may be of
+ * any number whose tensors span at most 2^46 elements, R = 0 included. `prec`
+ * may be RN18_FP16 too. Sums, statistics and the loss are fp32 or wider, and
+ * what is stored in 16 bits is rounded once, to nearest even. An output of
+ * the storage type may be an input itself (the same pointer and row stride);
+ * tensors must not overlap otherwise. Results do not depend on the order in
+ * which blocks run: the same inputs give the same bits. A workspace is
+ * scratch of one call (16-byte aligned, NULL where 0 bytes are needed): calls
+ * that may overlap need one each. RN18_ENOMEM if it is too small. */
+
+/* Layer norm over the D channels of each row (one pixel of an NHWC tensor):
+ *   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),
+ *   y = (x - mean) * rstd * gamma + beta
+ * gamma, beta fp32 [D] (NULL: 1 and 0); mean, rstd fp32 [R], kept for the
+ * backward pass (NULL in inference). A row that holds a NaN or an infinity
+ * gives NaN. */
+int rn18op_layernorm_fwd(int prec, const void* x, const float* gamma, const float* beta, void* y, float* mean,
+                         float* rstd, int64_t R, int D, int64_t ldx, int64_t ldy, float eps, void* hip_stream);
+
+/* Its backward pass, from the forward pass's input and statistics:
+ *   g = dy * gamma, xh = (x - mean) * rstd,
+ *   dx = rstd * (g - sum g / D - xh * sum(g * xh) / D),
+ *   dgamma = sum over rows of dy * xh, dbeta = sum over rows of dy
+ * dgamma, dbeta fp32 [D], overwritten (zeros for R = 0; either may be NULL,
+ * and without both no workspace is needed). dx may be dy or x itself. */
+size_t rn18op_layernorm_bwd_workspace(int prec, int64_t R, int D);
+int rn18op_layernorm_bwd(int prec, const void* dy, const void* x, const float* gamma, const float* mean,
+                         const float* rstd, void* dx, float* dgamma, float* dbeta, int64_t R, int D, int64_t lddy,
+                         int64_t ldx, int64_t lddx, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The K largest of the C logits of each row, 1 <= K <= min(C, 256):
+ *   vals fp32 [R][K] in descending order, idx int32 [R][K] their classes
+ * Equal values (the two zeros are equal) go in the order of their classes; a
+ * NaN is larger than every number. What a teacher keeps of its logits. */
+size_t rn18op_topk_logits_workspace(int prec, int64_t R, int C, int K);
+int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64_t R, int C, int64_t ldz, int K,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits, with the labels' cross-entropy,
+ * and the gradient of the student's logits z [R][C]:
+ *   P = softmax(z / T), p = softmax(z), q = softmax of t_vals / T over the
+ *   row's valid entries (0 <= t_idx < C and t_vals > -inf)
+ *   row_loss = w * (alpha T^2 sum_k q_k (log q_k - log P[t_idx_k])
+ *                   + (1 - alpha) (-log p[label]))
+ *   loss = scale * sum of row_loss
+ *   dz_j = scale * w * (alpha T (P_j - sum of q_k with t_idx_k = j)
+ *                       + (1 - alpha) (p_j - [j = label]))
+ * t_vals fp32, t_idx int32 [R][K], 0 <= K <= 256 (K = 0: both may be NULL), in
+ * any order; an entry that is not valid is left out (a short list is filled
+ * with t_idx = -1), and entries of one class add up. Terms with q_k = 0 are 0.
+ * A row without a valid entry has no soft term; one whose label is outside
+ * [0, C) (-1, say; labels NULL: every row) has no hard term; a row whose
+ * logits are all -inf (every class masked) has neither. Masked classes hold
+ * -inf and get a zero gradient. w: row_weight fp32 [R] (NULL: 1); a row of
+ * weight 0 has loss 0 and gradient 0 whatever its logits hold.
+ * row_loss fp32 [R]; loss 1 fp32 (may be NULL); dz as z (NULL: no gradient;
+ * may be z itself). temperature > 0, alpha in [0, 1], scale finite (1/R for
+ * the batch's mean, times a loss scale in fp16). */
+size_t rn18op_distill_loss_workspace(int prec, int64_t R, int C, int K);
+int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int32_t* t_idx, const int32_t* labels,
+                        const float* row_weight, void* dz, float* row_loss, float* loss, int64_t R, int C,
+                        int64_t ldz, int64_t lddz, int K, float temperature, float alpha, float scale,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Debugging aids (not part of the training path).
  * rn18_debug_set(ctx, RN18_DBG_STOP_BLOCKS, k): later train steps end their
  * backward pass after k residual blocks (no stem backward, no SGD update);

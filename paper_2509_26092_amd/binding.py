@@ -28,6 +28,8 @@ EXPORTED = [
     "rn18op_conv2d_fwd", "rn18op_conv2d_dgrad", "rn18op_conv2d_wgrad_workspace", "rn18op_conv2d_wgrad",
     "rn18op_maxpool_fwd", "rn18op_maxpool_bwd", "rn18_debug_set", "rn18_debug_copy",
     "rn18_debug_capture", "rn18op_round_bf16", "rn18op_conv2d_wgrad_noalloc_limit", "rn18op_conv2d_wgrad_noalloc",
+    "rn18op_layernorm_fwd", "rn18op_layernorm_bwd_workspace", "rn18op_layernorm_bwd",
+    "rn18op_topk_logits_workspace", "rn18op_topk_logits", "rn18op_distill_loss_workspace", "rn18op_distill_loss",
 ]
 
 
@@ -58,6 +60,7 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _Z = ctypes.c_size_t
 _F = ctypes.c_float
+_L = ctypes.c_int64
 
 
 def lib():
@@ -94,6 +97,14 @@ def lib():
         "rn18op_maxpool_fwd": (_I, [_I, _P, _P, _P, _I, _I, _I, _I, _P]),
         "rn18op_maxpool_bwd": (_I, [_I, _P, _P, _P, _I, _I, _I, _I, _P]),
         "rn18op_round_bf16": (_I, [_P, _P, _Z, _P]),
+        "rn18op_layernorm_fwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _F, _P]),
+        "rn18op_layernorm_bwd_workspace": (_Z, [_I, _L, _I]),
+        "rn18op_layernorm_bwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _L, _P, _Z, _P]),
+        "rn18op_topk_logits_workspace": (_Z, [_I, _L, _I, _I]),
+        "rn18op_topk_logits": (_I, [_I, _P, _P, _P, _L, _I, _L, _I, _P, _Z, _P]),
+        "rn18op_distill_loss_workspace": (_Z, [_I, _L, _I, _I]),
+        "rn18op_distill_loss": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _I, _F, _F, _F, _P, _Z,
+                                     _P]),
         "rn18_debug_set": (_I, [_P, _I, ctypes.c_long]),
         "rn18_profile_enable": (_I, [_P, _I]),
         "rn18_profile_read": (_I, [_P, ctypes.POINTER(rn18_prof_rec), _I, ctypes.POINTER(_I)]),
@@ -255,6 +266,47 @@ def rn18op_maxpool_bwd(prec, dy, arg, dx, N, H, W, C, stream=None):
 
 def rn18op_round_bf16(x, y, n, stream=None):
     return _check(lib().rn18op_round_bf16(_ptr(x), _ptr(y), n, _stream(stream)))
+
+
+def _ws(t):
+    """(pointer, bytes) of a workspace tensor or None."""
+    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
+
+
+def rn18op_layernorm_fwd(prec, x, gamma, beta, y, mean, rstd, R, D, ldx, ldy, eps=1e-5, stream=None):
+    return _check(lib().rn18op_layernorm_fwd(prec, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                             R, D, ldx, ldy, eps, _stream(stream)))
+
+
+def rn18op_layernorm_bwd_workspace(prec, R, D):
+    return lib().rn18op_layernorm_bwd_workspace(prec, R, D)
+
+
+def rn18op_layernorm_bwd(prec, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, R, D, lddy, ldx, lddx, ws=None,
+                         stream=None):
+    return _check(lib().rn18op_layernorm_bwd(prec, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx),
+                                             _ptr(dgamma), _ptr(dbeta), R, D, lddy, ldx, lddx, *_ws(ws),
+                                             _stream(stream)))
+
+
+def rn18op_topk_logits_workspace(prec, R, C, K):
+    return lib().rn18op_topk_logits_workspace(prec, R, C, K)
+
+
+def rn18op_topk_logits(prec, z, vals, idx, R, C, ldz, K, ws=None, stream=None):
+    return _check(lib().rn18op_topk_logits(prec, _ptr(z), _ptr(vals), _ptr(idx), R, C, ldz, K, *_ws(ws),
+                                           _stream(stream)))
+
+
+def rn18op_distill_loss_workspace(prec, R, C, K):
+    return lib().rn18op_distill_loss_workspace(prec, R, C, K)
+
+
+def rn18op_distill_loss(prec, z, t_vals, t_idx, labels, row_weight, dz, row_loss, loss, R, C, ldz, lddz, K,
+                        temperature, alpha, scale, ws=None, stream=None):
+    return _check(lib().rn18op_distill_loss(prec, _ptr(z), _ptr(t_vals), _ptr(t_idx), _ptr(labels), _ptr(row_weight),
+                                            _ptr(dz), _ptr(row_loss), _ptr(loss), R, C, ldz, lddz, K, temperature,
+                                            alpha, scale, *_ws(ws), _stream(stream)))
 
 
 DBG = dict(y=0, z1=1, out=2, gA=3, gB=4, gz=5, gy=6, gyd=7, grad=8, wf=9, wd=10, mean=11, rstd=12, zstem=13,

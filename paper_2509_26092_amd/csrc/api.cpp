@@ -1714,3 +1714,135 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* stream) {
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Row operators: layer norm, top logits, distillation
+// ---------------------------------------------------------------------------
+namespace {
+constexpr int64_t kMaxRowElems = (int64_t)1 << 46;   // rows x stride of one tensor
+
+// Rows x width of a tensor with row stride ld, elements of the storage type.
+int rows_check(int prec, const char* name, const void* p, int64_t R, int width, int64_t ld) {
+  if (ld < width) return fail(RN18_EINVAL, "the row stride of %s is below its width", name);
+  if (R > 0 && ld > kMaxRowElems / R) return fail(RN18_EINVAL, "%s spans more than 2^46 elements", name);
+  if (R > 0 && !p) return fail(RN18_EINVAL, "%s is NULL", name);
+  if ((uintptr_t)p & (uintptr_t)(prec_bytes(prec) - 1)) return fail(RN18_EINVAL, "%s is misaligned", name);
+  return RN18_OK;
+}
+int words_check(const char* name, const void* p, bool needed) {
+  if (needed && !p) return fail(RN18_EINVAL, "%s is NULL", name);
+  if ((uintptr_t)p & 3u) return fail(RN18_EINVAL, "%s is misaligned", name);
+  return RN18_OK;
+}
+// An output may replace an input, element for element.
+int alias_check(const char* name, const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t R) {
+  if (R > 1 && out && out == in && ldo != ldi)
+    return fail(RN18_EINVAL, "%s in place of its input needs the same row stride", name);
+  return RN18_OK;
+}
+int row_sizes_check(int prec, int64_t R, int width) {
+  if (prec != RN18_FP32 && prec != RN18_BF16 && prec != RN18_FP16) return fail(RN18_EINVAL, "bad precision");
+  if (R < 0 || R > kMaxRowElems) return fail(RN18_EINVAL, "bad number of rows");
+  if (width < 1) return fail(RN18_EINVAL, "non-positive size");
+  return RN18_OK;
+}
+int ws_check(const void* ws, size_t bytes, size_t need) {
+  if (!need) return RN18_OK;
+  if (!ws || !aligned16(ws)) return fail(RN18_EINVAL, "bad pointer");
+  if (bytes < need) return fail(RN18_ENOMEM, "workspace of %zu bytes, %zu needed", bytes, need);
+  return RN18_OK;
+}
+}  // namespace
+
+extern "C" {
+
+int rn18op_layernorm_fwd(int prec, const void* x, const float* gamma, const float* beta, void* y, float* mean,
+                         float* rstd, int64_t R, int D, int64_t ldx, int64_t ldy, float eps, void* stream) {
+  int r;
+  if ((r = row_sizes_check(prec, R, D)) || (r = rows_check(prec, "x", x, R, D, ldx)) ||
+      (r = rows_check(prec, "y", y, R, D, ldy)) || (r = alias_check("y", y, ldy, x, ldx, R)) ||
+      (r = words_check("gamma", gamma, false)) || (r = words_check("beta", beta, false)) ||
+      (r = words_check("mean", mean, false)) || (r = words_check("rstd", rstd, false)))
+    return r;
+  if (!(eps >= 0.f) || !isfinite(eps)) return fail(RN18_EINVAL, "eps must be finite and not negative");
+  LCHK(layernorm_fwd_launch(prec, x, gamma, beta, y, mean, rstd, R, D, ldx, ldy, eps, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+size_t rn18op_layernorm_bwd_workspace(int prec, int64_t R, int D) {
+  return row_sizes_check(prec, R, D) ? 0 : layernorm_bwd_workspace(prec, R, D);
+}
+
+int rn18op_layernorm_bwd(int prec, const void* dy, const void* x, const float* gamma, const float* mean,
+                         const float* rstd, void* dx, float* dgamma, float* dbeta, int64_t R, int D, int64_t lddy,
+                         int64_t ldx, int64_t lddx, void* ws, size_t ws_bytes, void* stream) {
+  int r;
+  if ((r = row_sizes_check(prec, R, D)) || (r = rows_check(prec, "dy", dy, R, D, lddy)) ||
+      (r = rows_check(prec, "x", x, R, D, ldx)) || (r = rows_check(prec, "dx", dx, R, D, lddx)) ||
+      (r = alias_check("dx", dx, lddx, dy, lddy, R)) || (r = alias_check("dx", dx, lddx, x, ldx, R)) ||
+      (r = words_check("gamma", gamma, false)) || (r = words_check("mean", mean, R > 0)) ||
+      (r = words_check("rstd", rstd, R > 0)) || (r = words_check("dgamma", dgamma, false)) ||
+      (r = words_check("dbeta", dbeta, false)))
+    return r;
+  if ((dgamma || dbeta) && (r = ws_check(ws, ws_bytes, layernorm_bwd_workspace(prec, R, D)))) return r;
+  LCHK(layernorm_bwd_launch(prec, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, R, D, lddy, ldx, lddx, ws,
+                            (hipStream_t)stream));
+  return RN18_OK;
+}
+
+static int topk_check(int prec, int64_t R, int C, int K) {
+  int r = row_sizes_check(prec, R, C);
+  if (r) return r;
+  if (K < 1 || K > C || K > kTopMax) return fail(RN18_EINVAL, "K must be in [1, min(C, %d)]", kTopMax);
+  return RN18_OK;
+}
+
+size_t rn18op_topk_logits_workspace(int prec, int64_t R, int C, int K) {
+  return topk_check(prec, R, C, K) ? 0 : topk_workspace(prec, R, C, K);
+}
+
+int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64_t R, int C, int64_t ldz, int K,
+                       void* ws, size_t ws_bytes, void* stream) {
+  int r;
+  if ((r = topk_check(prec, R, C, K)) || (r = rows_check(prec, "z", z, R, C, ldz)) ||
+      (r = words_check("vals", vals, R > 0)) || (r = words_check("idx", idx, R > 0)) ||
+      (r = ws_check(ws, ws_bytes, topk_workspace(prec, R, C, K))))
+    return r;
+  LCHK(topk_launch(prec, z, vals, idx, R, C, ldz, K, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+static int distill_check(int prec, int64_t R, int C, int K) {
+  int r = row_sizes_check(prec, R, C);
+  if (r) return r;
+  if (K < 0 || K > kTopMax) return fail(RN18_EINVAL, "K must be in [0, %d]", kTopMax);
+  return RN18_OK;
+}
+
+size_t rn18op_distill_loss_workspace(int prec, int64_t R, int C, int K) {
+  return distill_check(prec, R, C, K) ? 0 : distill_workspace(prec, R, C, K);
+}
+
+int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int32_t* t_idx, const int32_t* labels,
+                        const float* row_weight, void* dz, float* row_loss, float* loss, int64_t R, int C,
+                        int64_t ldz, int64_t lddz, int K, float temperature, float alpha, float scale, void* ws,
+                        size_t ws_bytes, void* stream) {
+  int r;
+  if ((r = distill_check(prec, R, C, K)) || (r = rows_check(prec, "z", z, R, C, ldz)) ||
+      (dz && (r = rows_check(prec, "dz", dz, R, C, lddz))) || (r = alias_check("dz", dz, lddz, z, ldz, R)) ||
+      (r = words_check("t_vals", t_vals, R > 0 && K > 0)) || (r = words_check("t_idx", t_idx, R > 0 && K > 0)) ||
+      (r = words_check("labels", labels, false)) || (r = words_check("row_weight", row_weight, false)) ||
+      (r = words_check("row_loss", row_loss, R > 0)) || (r = words_check("loss", loss, false)))
+    return r;
+  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.0f / temperature))
+    return fail(RN18_EINVAL, "the temperature must be positive and finite");
+  if (!(alpha >= 0.f && alpha <= 1.f)) return fail(RN18_EINVAL, "alpha must be in [0, 1]");
+  if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
+  if ((r = ws_check(ws, ws_bytes, distill_workspace(prec, R, C, K)))) return r;
+  const DistillArgs a{z, t_vals, t_idx, labels, row_weight, dz, row_loss, R, ldz, lddz, C, K, temperature, alpha,
+                      scale};
+  LCHK(distill_launch(prec, a, loss, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+}  // extern "C"

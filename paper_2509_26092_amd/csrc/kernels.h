@@ -272,4 +272,37 @@ int merge_launch(float* p, const float* ds, const float* dl, long n, float f, hi
 int delta_launch(const float* pulled, const float* local, float* delta, long n, hipStream_t s);
 int fill_zero_launch(void* p, size_t bytes, hipStream_t s);
 
+// Layer norm of R rows of D channels (row strides in elements), forward and
+// backward; the backward pass needs layernorm_bwd_workspace bytes at ws.
+int layernorm_fwd_launch(int prec, const void* x, const float* gamma, const float* beta, void* y, float* mean,
+                         float* rstd, long R, int D, long ldx, long ldy, float eps, hipStream_t s);
+size_t layernorm_bwd_workspace(int prec, long R, int D);
+int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* gamma, const float* mean,
+                         const float* rstd, void* dx, float* dgamma, float* dbeta, long R, int D, long lddy, long ldx,
+                         long lddx, void* ws, hipStream_t s);
+
+// The K largest logits of R rows over C classes and their classes, in
+// descending order; K at most kTopMax, topk_workspace bytes at ws.
+constexpr int kTopMax = 256;
+size_t topk_workspace(int prec, long R, int C, int K);
+int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int C, long ldz, int K, void* ws,
+                hipStream_t s);
+
+// Distillation against a teacher's top logits. labels, weight and dz may be
+// NULL; loss (optional) is written with scale * sum of the row losses.
+struct DistillArgs {
+  const void* z;
+  const float* t_vals;
+  const int32_t* t_idx;
+  const int32_t* labels;
+  const float* weight;
+  void* dz;
+  float* row_loss;
+  long R, ldz, lddz;
+  int C, K;
+  float temperature, alpha, scale;
+};
+size_t distill_workspace(int prec, long R, int C, int K);
+int distill_launch(int prec, const DistillArgs& a, float* loss, void* ws, hipStream_t s);
+
 }  // namespace rn18

@@ -1,0 +1,591 @@
+"""GPU parity of the row operators (layer norm, top logits, distillation loss)
+with the fp64 oracle, through the C ABI: every storage type, widths from one
+to beyond what a block keeps in registers, row strides, misaligned rows,
+outputs in place of inputs, masked rows and classes, NaN and infinities,
+offsets beyond 32 bits, streams and graph replays.
+
+Tolerances. U is the unit roundoff of the stored type (0 for fp32); fp32
+arithmetic adds TOL = 1e-5 of the largest value (a few roundings of 2^-24
+each, times arguments of exponentials up to about 40)."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import rows
+from paper_2509_26092_amd import binding as B
+from gpu_util import PREC, assert_close, rounded, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+PRECS = ["fp32", "bf16", "fp16"]
+U = {"fp32": 0.0, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+TOL = 1e-5
+EPS = 1e-5
+
+
+def mat(a, prec, pad=0, off=0, fill=float("nan")):
+    """A numpy matrix as a device view with `pad` elements between the rows
+    and `off` elements before the first, and the buffer that holds it."""
+    import torch
+    R, D = a.shape
+    buf = torch.full((off + R * (D + pad) + 64,), fill, dtype=torch_dtype(prec), device="cuda")
+    v = torch.as_strided(buf, (R, D), (D + pad, 1), off)
+    v.copy_(torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda())
+    return v, buf
+
+
+def out(R, D, prec, pad=0, off=0):
+    return mat(np.full((R, D), 7.0), prec, pad, off, fill=-3.0)
+
+
+def gaps_kept(v, buf):
+    """Nothing outside the view was written (the buffer was filled with -3)."""
+    b = buf.clone()
+    import torch
+    torch.as_strided(b, v.shape, v.stride(), v.storage_offset()).fill_(-3.0)
+    return bool((b == -3.0).all())
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def vec(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+
+
+def empty(n, dtype=None):
+    import torch
+    return torch.full((n,), -9.0, device="cuda").to(dtype or torch.float32)
+
+
+def ws_of(n):
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
+
+
+# (rows, width, x pad, y pad, offset)
+LN_SHAPES = [(1, 1, 0, 0, 0), (5, 1, 2, 0, 1), (1, 7, 0, 0, 0), (3, 64, 0, 0, 0), (1001, 16, 0, 0, 0),
+             (70000, 8, 0, 0, 0), (517, 63, 0, 0, 0), (130, 65, 3, 1, 1), (64, 512, 0, 0, 0), (257, 520, 8, 16, 8),
+             (33, 1000, 0, 0, 0), (9, 1023, 1, 0, 3), (700, 2050, 7, 0, 0), (5, 4097, 0, 3, 0), (300, 8192, 0, 0, 0),
+             (2, 16384, 0, 0, 0), (3, 16390, 2, 0, 1), (2, 33000, 0, 0, 0), (1, 70001, 0, 0, 0)]
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,D,px,py,off", LN_SHAPES)
+def test_layernorm_fwd(prec, R, D, px, py, off):
+    import torch
+    rng = np.random.default_rng(R * 131 + D)
+    x = rounded(rng.standard_normal((R, D)) * 1.5 + 0.4, prec)
+    gamma, beta = (rng.standard_normal(D).astype(np.float32) for _ in range(2))
+    xd, _ = mat(x, prec, px, off)
+    for g, b in ((gamma, beta), (None, beta), (gamma, None)):
+        yd, ybuf = out(R, D, prec, py, off)
+        mean, rstd = empty(R), empty(R)
+        B.rn18op_layernorm_fwd(PREC[prec], xd, None if g is None else vec(g), None if b is None else vec(b), yd, mean,
+                               rstd, R, D, D + px, D + py, EPS)
+        torch.cuda.synchronize()
+        y, m, rs = rows.layernorm_forward(x, g, b, EPS)
+        assert_close(f64(yd), y, U[prec] + TOL, "y")
+        assert_close(f64(mean), m, TOL, "mean")
+        assert_close(f64(rstd), rs, TOL, "rstd")
+        assert gaps_kept(yd, ybuf)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,D", [(7, 64), (1, 513), (40, 1000), (6, 16384), (2, 70001)])
+def test_layernorm_fwd_in_place_without_statistics(prec, R, D):
+    import torch
+    rng = np.random.default_rng(D)
+    x = rounded(rng.standard_normal((R, D)), prec)
+    xd, _ = mat(x, prec)
+    B.rn18op_layernorm_fwd(PREC[prec], xd, None, None, xd, None, None, R, D, D, D, EPS)
+    torch.cuda.synchronize()
+    assert_close(f64(xd), rows.layernorm_forward(x, None, None, EPS)[0], U[prec] + TOL, "y")
+
+
+def test_layernorm_fwd_rows_far_from_zero():
+    """Mean 100, deviation 1: the mean's rounding (2^-24 of 100, a few times)
+    is what is left in y."""
+    import torch
+    rng = np.random.default_rng(5)
+    for R, D in ((50, 64), (20, 1000), (3, 8192), (2, 70001)):
+        x = rounded(rng.standard_normal((R, D)) + 100.0, "fp32")
+        xd, _ = mat(x, "fp32")
+        yd, _ = out(R, D, "fp32")
+        B.rn18op_layernorm_fwd(B.RN18_FP32, xd, None, None, yd, None, None, R, D, D, D, EPS)
+        torch.cuda.synchronize()
+        y = rows.layernorm_forward(x, None, None, EPS)[0]
+        assert np.abs(f64(yd) - y).max() <= 1e-5 * np.abs(y).max() + 8 * 100 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("D", [8, 65, 512, 8192, 33000])
+def test_layernorm_constant_and_non_finite_rows(prec, D):
+    """A constant row gives beta; a NaN or an infinity stays in its row."""
+    import torch
+    R = 12
+    rng = np.random.default_rng(D)
+    x = rounded(rng.standard_normal((R, D)), prec)
+    x[1] = 3.0
+    x[4, D // 2], x[7, 0], x[9, D - 1] = np.nan, np.inf, -np.inf
+    bad = [4, 7, 9]
+    good = [r for r in range(R) if r not in bad]
+    beta = rng.standard_normal(D).astype(np.float32)
+    xd, _ = mat(x, prec)
+    yd, _ = out(R, D, prec)
+    B.rn18op_layernorm_fwd(PREC[prec], xd, None, vec(beta), yd, None, None, R, D, D, D, EPS)
+    torch.cuda.synchronize()
+    y = f64(yd)
+    assert np.isnan(y[bad]).all()
+    assert_close(y[good], rows.layernorm_forward(x[good], None, beta, EPS)[0], U[prec] + TOL, "y")
+
+
+def ln_bwd_case(prec, R, D, pdy=0, px=0, pdx=0, off=0, seed=0):
+    rng = np.random.default_rng(R * 17 + D + seed)
+    x = rounded(rng.standard_normal((R, D)) * 1.5 + 0.4, prec)
+    dy = rounded(rng.standard_normal((R, D)) * 0.7, prec)
+    gamma = rng.standard_normal(D).astype(np.float32)
+    _, m, rs = rows.layernorm_forward(x, None, None, EPS)
+    m, rs = m.astype(np.float32), rs.astype(np.float32)
+    return x, dy, gamma, m, rs
+
+
+def check_param_grads(dgamma, dbeta, dy, x, m, rs):
+    """Sums over R rows in fp32, in chains of at most R additions: the partial
+    sums of random terms grow like the root of their number, so their
+    roundings add up to about R 2^-24 rms(term); four times that, and the
+    terms' own roundings."""
+    R = len(dy)
+    xh = (x - m[:, None].astype(np.float64)) * rs[:, None].astype(np.float64)
+    for got, terms, name in ((dgamma, dy * xh, "dgamma"), (dbeta, dy, "dbeta")):
+        if got is None:
+            continue
+        rms = np.sqrt((terms ** 2).mean(axis=0))
+        err = np.abs(f64(got) - terms.sum(axis=0))
+        assert (err <= 4 * R * 2.0 ** -24 * rms + 16 * math.sqrt(R) * 2.0 ** -24 * (rms + rms.max())).all(), \
+            (name, (err / (rms + 1e-30)).max())
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,D,px,py,off", LN_SHAPES)
+def test_layernorm_bwd(prec, R, D, px, py, off):
+    import torch
+    x, dy, gamma, m, rs = ln_bwd_case(prec, R, D)
+    xd, _ = mat(x, prec, px, off)
+    dyd, _ = mat(dy, prec, py, off)
+    dxd, dxbuf = out(R, D, prec, px + py, off)
+    dgamma, dbeta = empty(D), empty(D)
+    ws = ws_of(B.rn18op_layernorm_bwd_workspace(PREC[prec], R, D))
+    B.rn18op_layernorm_bwd(PREC[prec], dyd, xd, vec(gamma), vec(m), vec(rs), dxd, dgamma, dbeta, R, D, D + py, D + px,
+                           D + px + py, ws)
+    torch.cuda.synchronize()
+    dx = rows.layernorm_backward(dy, x, gamma, m, rs)[0]
+    # dx is a difference of terms of the size of rs * dy * gamma: its roundings are relative to those
+    size = np.abs(rs[:, None] * dy * gamma).max()
+    err = np.abs(f64(dxd) - dx)
+    assert (err <= U[prec] * np.abs(dx) + TOL * size).all(), err.max() / size
+    check_param_grads(dgamma, dbeta, dy, x, m, rs)
+    assert gaps_kept(dxd, dxbuf)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,D", [(9, 64), (300, 513), (40, 4096), (3, 33000)])
+@pytest.mark.parametrize("place", ["dy", "x"])
+def test_layernorm_bwd_in_place_and_partial_outputs(prec, R, D, place):
+    """dx in place of dy or of x; without gamma; each parameter gradient alone
+    and none; every result as in the full call, bit for bit."""
+    import torch
+    x, dy, _, m, rs = ln_bwd_case(prec, R, D, seed=3)
+    ws = ws_of(B.rn18op_layernorm_bwd_workspace(PREC[prec], R, D))
+    ref = None
+    for want_g, want_b in ((True, True), (True, False), (False, True), (False, False)):
+        xd, _ = mat(x, prec)
+        dyd, _ = mat(dy, prec)
+        dxd = dyd if place == "dy" else xd
+        dgamma, dbeta = empty(D) if want_g else None, empty(D) if want_b else None
+        B.rn18op_layernorm_bwd(PREC[prec], dyd, xd, None, vec(m), vec(rs), dxd, dgamma, dbeta, R, D, D, D, D,
+                               ws if want_g or want_b else None)
+        torch.cuda.synchronize()
+        if ref is None:
+            ref = dxd.clone()
+            dx = rows.layernorm_backward(dy, x, None, m, rs)[0]
+            size = np.abs(rs[:, None] * dy).max()
+            assert (np.abs(f64(dxd) - dx) <= U[prec] * np.abs(dx) + TOL * size).all()
+        assert torch.equal(ref, dxd)
+        check_param_grads(dgamma, dbeta, dy, x, m, rs)
+
+
+def test_layernorm_gradient_against_differences_of_the_operator():
+    """The forward operator itself, moved by +-h along random directions of
+    x, gamma and beta in fp32: f = sum dy y is about 1e2 with an error of
+    1e-6, so at h = 1e-2 the quotient is good to 1e-3 of the gradient's norm."""
+    import torch
+    R, D, h = 16, 96, 1e-2
+    x, dy, gamma, m, rs = ln_bwd_case("fp32", R, D, seed=9)
+    rng = np.random.default_rng(11)
+    beta = rng.standard_normal(D)
+    d = {"x": rng.standard_normal((R, D)), "gamma": rng.standard_normal(D), "beta": rng.standard_normal(D)}
+    for k in d:
+        d[k] /= np.linalg.norm(d[k])
+
+    def f(s):
+        xd, _ = mat(x + s * d["x"], "fp32")
+        yd, _ = out(R, D, "fp32")
+        B.rn18op_layernorm_fwd(B.RN18_FP32, xd, vec(gamma + s * d["gamma"]), vec(beta + s * d["beta"]), yd, None, None,
+                               R, D, D, D, EPS)
+        return float((f64(yd) * dy).sum())
+
+    xd, _ = mat(x, "fp32")
+    dyd, _ = mat(dy, "fp32")
+    dxd, _ = out(R, D, "fp32")
+    dgamma, dbeta = empty(D), empty(D)
+    B.rn18op_layernorm_bwd(B.RN18_FP32, dyd, xd, vec(gamma), vec(m), vec(rs), dxd, dgamma, dbeta, R, D, D, D, D,
+                           ws_of(B.rn18op_layernorm_bwd_workspace(B.RN18_FP32, R, D)))
+    slope = (f64(dxd) * d["x"]).sum() + (f64(dgamma) * d["gamma"]).sum() + (f64(dbeta) * d["beta"]).sum()
+    norm = math.sqrt((f64(dxd) ** 2).sum() + (f64(dgamma) ** 2).sum() + (f64(dbeta) ** 2).sum())
+    assert abs((f(h) - f(-h)) / (2 * h) - slope) <= 1e-3 * norm
+
+
+# ---------------------------------------------------------------- top logits
+def run_topk(zd, prec, R, C, K, ld):
+    import torch
+    vals = torch.full((R, K), -9.0, device="cuda")
+    idx = torch.full((R, K), -9, dtype=torch.int32, device="cuda")
+    ws = ws_of(B.rn18op_topk_logits_workspace(PREC[prec], R, C, K))
+    B.rn18op_topk_logits(PREC[prec], zd, vals, idx, R, C, ld, K, ws)
+    torch.cuda.synchronize()
+    return vals.cpu().numpy(), idx.cpu().numpy()
+
+
+def check_topk(z, prec, K, pad=0, off=0):
+    R, C = z.shape
+    zd, _ = mat(z, prec, pad, off)
+    vals, idx = run_topk(zd, prec, R, C, K, C + pad)
+    v, i = rows.topk(z, K)
+    assert np.array_equal(idx, i)
+    assert np.array_equal(vals.astype(np.float64), v, equal_nan=True)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,C,K,pad,off", [(1, 1, 1, 0, 0), (3, 2, 2, 0, 0), (70, 10, 3, 0, 0), (9, 10, 10, 1, 1),
+                                           (5, 63, 63, 0, 0), (5, 64, 64, 0, 0), (31, 100, 5, 3, 1), (4, 257, 256, 0, 0),
+                                           (256, 1000, 10, 0, 0), (7, 1000, 100, 0, 5), (2, 1001, 256, 7, 1),
+                                           (300, 2048, 1, 0, 0), (5, 4097, 33, 0, 0), (3, 16384, 256, 0, 0),
+                                           (20, 32768, 64, 0, 0), (2, 40001, 20, 1, 3), (2, 131071, 256, 0, 1),
+                                           (1, 131072, 8, 0, 0), (1, 300001, 64, 0, 0)])
+def test_topk(prec, R, C, K, pad, off):
+    rng = np.random.default_rng(C + K)
+    check_topk(rounded(rng.standard_normal((R, C)) * 2.5, prec), prec, K, pad, off)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("C,K", [(10, 10), (100, 7), (1000, 64), (1000, 200), (5000, 256), (40000, 64), (131072, 256)])
+def test_topk_ties_orders_and_special_values(prec, C, K):
+    """Rows whose top entries crowd in one place: equal values everywhere,
+    ascending and descending rows, one run of large values, few distinct
+    values, both zeros, all masked but some, all masked, NaN and infinities,
+    the type's lowest and highest values."""
+    rng = np.random.default_rng(C)
+    hi = {"fp32": 3.4028234663852886e38, "bf16": 3.3895313892515355e38, "fp16": 65504.0}[prec]
+    ramp = rounded(np.linspace(-4.0, 4.0, C), prec)
+    run = rounded(rng.standard_normal(C), prec)
+    run[C // 3:C // 3 + min(K + 5, C // 2)] += 16.0
+    few = rng.integers(0, 3, C).astype(np.float64)
+    zeros = np.where(rng.random(C) < 0.5, 0.0, -0.0)
+    masked = np.full(C, -np.inf)
+    masked[rng.integers(0, C, max(1, K // 2))] = 1.0
+    odd = rounded(rng.standard_normal(C), prec)
+    odd[rng.integers(0, C, 3)] = np.nan
+    odd[rng.integers(0, C, 3)] = np.inf
+    odd[rng.integers(0, C, 3)] = hi
+    low = np.full(C, -hi)
+    low[C - 1] = -np.inf
+    z = np.stack([np.full(C, 1.0), ramp, ramp[::-1], rounded(run, prec), few, zeros, masked, np.full(C, -np.inf), odd,
+                  np.full(C, np.nan), low])
+    check_topk(z, prec, K)
+
+
+# ---------------------------------------------------------------- distillation
+def distill_inputs(prec, R, C, K, masked, seed=0):
+    rng = np.random.default_rng(R + 7 * C + 31 * K + seed)
+    z = rounded(rng.standard_normal((R, C)) * 2.5, prec)
+    t_idx = rng.integers(0, C, (R, K)).astype(np.int32)      # with doubled classes
+    t_vals = (np.take_along_axis(z, t_idx.astype(np.int64), 1) + rng.standard_normal((R, K))).astype(np.float32)
+    labels = rng.integers(0, C, R).astype(np.int32)
+    weight = None
+    if K and R > 1:
+        labels[0] = t_idx[0, 0]                               # a label that the list names too
+    if masked:
+        weight = (0.5 + rng.random(R)).astype(np.float32)
+        weight[rng.random(R) < 0.15] = 0.0
+        labels[rng.random(R) < 0.2] = -1
+        labels[rng.random(R) < 0.1] = C
+        t_idx[rng.random((R, K)) < 0.2] = -1
+        t_idx[rng.random((R, K)) < 0.05] = C
+        t_idx[rng.random(R) < 0.1] = -1
+        t_vals[rng.random((R, K)) < 0.1] = -np.inf
+        used = set(t_idx.ravel().tolist()) | set(labels.tolist())
+        hidden = [c for c in rng.integers(0, C, C // 20) if c not in used]
+        z[:, hidden] = -np.inf
+        z[weight == 0.0] = np.nan
+        for r in np.flatnonzero(rng.random(R) < 0.05):
+            z[r] = -np.inf
+    return z, t_vals, t_idx, labels, weight
+
+
+def run_distill(zd, prec, t_vals, t_idx, labels, weight, K, T, alpha, scale, R, C, ldz, dzd=None, lddz=0,
+                want_loss=True):
+    import torch
+    row_loss, loss = empty(R), empty(1) if want_loss else None
+    tv = vec(t_vals) if K else None
+    ti = torch.from_numpy(np.ascontiguousarray(t_idx)).cuda() if K else None
+    lab = None if labels is None else torch.from_numpy(labels).cuda()
+    w = None if weight is None else vec(weight)
+    ws = ws_of(B.rn18op_distill_loss_workspace(PREC[prec], R, C, K))
+    B.rn18op_distill_loss(PREC[prec], zd, tv, ti, lab, w, dzd, row_loss, loss, R, C, ldz, lddz, K, T, alpha, scale, ws)
+    torch.cuda.synchronize()
+    return f64(row_loss), None if loss is None else float(loss.item())
+
+
+def loss_bound(z, t_vals, w, T, alpha):
+    """log q and log P are differences of terms of at most M: eight roundings
+    of 2^-24 of them, and as much for the sums of exponentials."""
+    fin = np.abs(z[np.isfinite(z)])
+    t = np.abs(t_vals[np.isfinite(t_vals)])
+    M = (max(fin.max() if fin.size else 0.0, t.max() if t.size else 0.0)) * max(1.0, 1.0 / T) + np.log(z.shape[1]) + 4
+    return (alpha * T * T + 1 - alpha) * M * 2.0 ** -21 * (1.0 if w is None else w.max())
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,C,K,T,alpha,masked,pad,off",
+                         [(1, 1, 1, 1.0, 0.5, False, 0, 0), (3, 2, 0, 2.0, 0.0, False, 0, 0),
+                          (65, 10, 4, 4.0, 0.9, False, 0, 0), (64, 10, 4, 2.0, 0.4, True, 1, 1),
+                          (9, 100, 100, 3.0, 1.0, False, 0, 0), (40, 100, 7, 1.0, 0.5, True, 0, 0),
+                          (64, 1000, 10, 4.0, 0.9, False, 0, 0), (50, 1000, 256, 1.5, 0.7, True, 3, 1),
+                          (7, 1023, 33, 2.0, 1.0, True, 1, 0), (5, 2048, 64, 0.5, 0.3, False, 0, 0),
+                          (30, 5001, 20, 2.0, 0.5, True, 3, 0), (6, 16384, 64, 2.0, 1.0, False, 0, 8),
+                          (3, 32768, 64, 2.5, 0.6, True, 0, 0), (2, 50001, 32, 1.5, 0.5, True, 3, 1),
+                          (1, 131071, 20, 2.0, 1.0, False, 0, 1), (2, 131072, 8, 6.0, 0.5, False, 0, 0),
+                          (1, 300001, 64, 2.0, 0.5, False, 0, 0)])
+def test_distill(prec, R, C, K, T, alpha, masked, pad, off):
+    z, t_vals, t_idx, labels, weight = distill_inputs(prec, R, C, K, masked)
+    scale = (1024.0 if prec == "fp16" else 1.0) / R
+    zd, _ = mat(z, prec, pad, off)
+    dzd, dzbuf = out(R, C, prec, 2 * pad, off)
+    row, loss = run_distill(zd, prec, t_vals, t_idx, labels, weight, K, T, alpha, scale, R, C, C + pad, dzd,
+                            C + 2 * pad)
+    row_o, loss_o, dz_o = rows.distill(z, t_vals, t_idx, labels, weight, T, alpha, scale)
+    tol = loss_bound(z, t_vals, weight, T, alpha)
+    assert np.abs(row - row_o).max() <= tol
+    assert abs(loss - loss_o) <= scale * R * tol + 2.0 ** -23 * abs(loss_o)
+    if np.abs(dz_o).max() > 1e-9:
+        assert_close(f64(dzd), dz_o, U[prec] + TOL, "dz")
+    else:     # one class: nothing to learn
+        assert np.abs(f64(dzd)).max() <= scale * T * TOL
+    assert gaps_kept(dzd, dzbuf)
+    if weight is not None:
+        assert not f64(dzd)[weight == 0.0].any()
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,C,K", [(12, 10, 3), (20, 1000, 40), (3, 33000, 64), (1, 131072, 16), (1, 300001, 5)])
+def test_distill_in_place_and_loss_alone(prec, R, C, K):
+    """dz in place of z, and the loss without a gradient: bit for bit what
+    the full call gives, and the same again on a second call."""
+    import torch
+    z, t_vals, t_idx, labels, weight = distill_inputs(prec, R, C, K, R > 1, seed=5)
+    a = (t_vals, t_idx, labels, weight, K, 2.0, 0.5, 1.0, R, C, C)
+    zd, _ = mat(z, prec)
+    dzd, _ = out(R, C, prec)
+    row, loss = run_distill(zd, prec, *a, dzd, C)
+    dz2, _ = out(R, C, prec)
+    row2, loss2 = run_distill(zd, prec, *a, dz2, C)
+    assert torch.equal(dzd, dz2) and np.array_equal(row, row2) and loss == loss2
+    row3, loss3 = run_distill(zd, prec, *a)
+    assert np.array_equal(row, row3) and loss == loss3
+    row4, _ = run_distill(zd, prec, *a, zd, C, want_loss=False)
+    assert torch.equal(dzd, zd) and np.array_equal(row, row4)
+
+
+@pytest.mark.parametrize("C", [10, 1000, 33000, 131072, 200000])
+def test_distill_extreme_logits(C):
+    """Rows where exponentials under- or overflow without the maximum taken
+    out: a class far above the others, all at the type's lowest value, one
+    infinite. A masked class with a share of the teacher's word has an
+    infinite loss and a finite gradient; NaN and +inf stay in their row."""
+    import torch
+    R, K, T = 7, 2, 2.0
+    z = np.zeros((R, C))
+    z[0, 3] = 3e4
+    z[1] = -3.4028234663852886e38
+    z[2] = -3.4028234663852886e38
+    z[2, 5] = 0.0
+    z[3, 1] = -np.inf
+    z[4, 2] = np.nan
+    z[5, 2] = np.inf
+    z[6, 2:] = -np.inf
+    t_idx = np.tile(np.array([[1, 5]], np.int32), (R, 1))
+    t_idx[6] = [0, 1]
+    t_vals = np.zeros((R, K), np.float32)
+    zd, _ = mat(z, "fp32")
+    dzd, _ = out(R, C, "fp32")
+    row, loss = run_distill(zd, "fp32", t_vals, t_idx, None, None, K, T, 1.0, 1.0, R, C, C, dzd, C)
+    dz = f64(dzd)
+    fin = [0, 1, 2, 6]
+    with np.errstate(all="ignore"):
+        row_o, _, dz_o = rows.distill(z, t_vals, t_idx, None, None, T, 1.0, 1.0)
+    assert np.allclose(row[fin], row_o[fin], rtol=1e-5, atol=1e-6)
+    assert_close(dz[[0, 1, 2, 3, 6]], dz_o[[0, 1, 2, 3, 6]], TOL, "dz")
+    assert row[3] == np.inf
+    assert np.isnan(row[4:6]).all() and np.isnan(dz[4:6]).all() and np.isnan(loss)
+
+
+def test_distill_gradient_against_differences_of_the_operator():
+    """The loss itself, moved by +-h along random directions in fp32: it is
+    about 1 with an error of 1e-6, so at h = 1e-2 the quotient is good to
+    1e-4 plus truncation, 1e-3 of the gradient's norm."""
+    R, C, K, T, alpha, h = 4, 50, 8, 2.0, 0.6, 1e-2
+    z, t_vals, t_idx, labels, _ = distill_inputs("fp32", R, C, K, False, seed=8)
+    dzd, _ = out(R, C, "fp32")
+    zd, _ = mat(z, "fp32")
+    run_distill(zd, "fp32", t_vals, t_idx, labels, None, K, T, alpha, 1.0, R, C, C, dzd, C)
+    g = f64(dzd)
+    rng = np.random.default_rng(4)
+    for _ in range(4):
+        d = rng.standard_normal((R, C))
+        d /= np.linalg.norm(d)
+        up, _ = mat(z + h * d, "fp32")
+        dn, _ = mat(z - h * d, "fp32")
+        lu = run_distill(up, "fp32", t_vals, t_idx, labels, None, K, T, alpha, 1.0, R, C, C)[0].sum()
+        ld = run_distill(dn, "fp32", t_vals, t_idx, labels, None, K, T, alpha, 1.0, R, C, C)[0].sum()
+        assert abs((lu - ld) / (2 * h) - (g * d).sum()) <= 1e-3 * max(1.0, np.linalg.norm(g))
+
+
+# ---------------------------------------------------------------- all of them
+def test_no_rows():
+    """R = 0: nothing is read or written but the sums over no rows."""
+    import torch
+    dgamma, dbeta, loss = empty(9), empty(9), empty(1)
+    ws = ws_of(max(16, B.rn18op_layernorm_bwd_workspace(B.RN18_FP32, 0, 9),
+                   B.rn18op_topk_logits_workspace(B.RN18_FP32, 0, 9, 3),
+                   B.rn18op_distill_loss_workspace(B.RN18_FP32, 0, 9, 3)))
+    B.rn18op_layernorm_fwd(B.RN18_FP32, None, None, None, None, None, None, 0, 9, 9, 9)
+    B.rn18op_layernorm_bwd(B.RN18_FP32, None, None, None, None, None, None, dgamma, dbeta, 0, 9, 9, 9, 9, ws)
+    B.rn18op_topk_logits(B.RN18_FP32, None, None, None, 0, 9, 9, 3, ws)
+    B.rn18op_distill_loss(B.RN18_FP32, None, None, None, None, None, None, None, loss, 0, 9, 9, 9, 3, 2.0, 0.5, 1.0, ws)
+    torch.cuda.synchronize()
+    assert not dgamma.any() and not dbeta.any() and loss.item() == 0.0
+
+
+@pytest.mark.parametrize("W", [64, 1000, 40000])
+def test_rows_beyond_32_bit_offsets(W):
+    """Three rows 2^31 + 8 elements apart (8.6 GB in bf16): byte and element
+    offsets pass 32 bits. One buffer; inputs at its start, outputs W
+    elements on."""
+    import torch
+    R, ld = 3, 2 ** 31 + 8
+    rng = np.random.default_rng(W)
+    x = rounded(rng.standard_normal((R, W)), "bf16")
+    dy = rounded(rng.standard_normal((R, W)), "bf16")
+    buf = torch.empty(2 * ld + 4 * W, dtype=torch.bfloat16, device="cuda")
+
+    def view(i):
+        return torch.as_strided(buf, (R, W), (ld, 1), i * W)
+
+    view(0).copy_(torch.from_numpy(x))
+    view(1).copy_(torch.from_numpy(dy))
+    mean, rstd = empty(R), empty(R)
+    B.rn18op_layernorm_fwd(B.RN18_BF16, view(0), None, None, view(2), mean, rstd, R, W, ld, ld, EPS)
+    y, m, rs = rows.layernorm_forward(x, None, None, EPS)
+    assert_close(f64(view(2)), y, U["bf16"] + TOL, "y")
+    dgamma, dbeta = empty(W), empty(W)
+    B.rn18op_layernorm_bwd(B.RN18_BF16, view(1), view(0), None, mean, rstd, view(2), dgamma, dbeta, R, W, ld, ld, ld,
+                           ws_of(B.rn18op_layernorm_bwd_workspace(B.RN18_BF16, R, W)))
+    dx = rows.layernorm_backward(dy, x, None, m, rs)[0]
+    assert (np.abs(f64(view(2)) - dx) <= U["bf16"] * np.abs(dx) + TOL * np.abs(rs[:, None] * dy).max()).all()
+    check_param_grads(dgamma, dbeta, dy, x, m, rs)
+    vals, idx = run_topk(view(0), "bf16", R, W, 5, ld)
+    v, i = rows.topk(x, 5)
+    assert np.array_equal(idx, i) and np.array_equal(vals, v)
+    row, _ = run_distill(view(0), "bf16", vals, idx, None, None, 5, 2.0, 1.0, 1.0, R, W, ld, view(2), ld)
+    row_o, _, dz_o = rows.distill(x, vals, idx, None, None, 2.0, 1.0, 1.0)
+    assert np.abs(row - row_o).max() <= loss_bound(x, vals, None, 2.0, 1.0)
+    assert_close(f64(view(2)), dz_o, U["bf16"] + TOL, "dz")
+    assert torch.equal(view(0).cpu(), torch.from_numpy(x).to(torch.bfloat16))
+
+
+def _chain(prec, R, W, K, seed):
+    """Buffers and a function that runs every operator on them."""
+    import torch
+    x, dy, gamma, m, rs = ln_bwd_case(prec, R, W, seed=seed)
+    xd, dyd = mat(x, prec)[0], mat(dy, prec)[0]
+    g = vec(gamma)
+    y, dx, dz = (out(R, W, prec)[0] for _ in range(3))
+    mean, rstd, dgamma, dbeta, row, loss = empty(R), empty(R), empty(W), empty(W), empty(R), empty(1)
+    vals = torch.zeros((R, K), device="cuda")
+    idx = torch.zeros((R, K), dtype=torch.int32, device="cuda")
+    lab = torch.arange(R, device="cuda", dtype=torch.int32) % W
+    p = PREC[prec]
+    w1, w2, w3 = (ws_of(n) for n in (B.rn18op_layernorm_bwd_workspace(p, R, W), B.rn18op_topk_logits_workspace(p, R, W, K),
+                                     B.rn18op_distill_loss_workspace(p, R, W, K)))
+
+    def go():
+        B.rn18op_layernorm_fwd(p, xd, g, None, y, mean, rstd, R, W, W, W, EPS)
+        B.rn18op_topk_logits(p, dyd, vals, idx, R, W, W, K, w2)
+        B.rn18op_distill_loss(p, y, vals, idx, lab, None, dz, row, loss, R, W, W, W, K, 2.0, 0.5, 1.0, w3)
+        B.rn18op_layernorm_bwd(p, dz, xd, g, mean, rstd, dx, dgamma, dbeta, R, W, W, W, W, w1)
+
+    return go, [y, mean, rstd, vals, idx, dz, row, loss, dx, dgamma, dbeta], xd
+
+
+@pytest.mark.parametrize("prec,R,W,K", [("bf16", 200, 1000, 10), ("fp32", 3, 40000, 33), ("fp16", 1, 131072, 64),
+                                        ("bf16", 5000, 64, 4)])
+def test_two_streams_and_repeats_give_the_same_bits(prec, R, W, K):
+    """Two chains on two streams at once, each with its own workspaces, and
+    again one after the other."""
+    import torch
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    a, b = _chain(prec, R, W, K, 1), _chain(prec, R, W, K, 2)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            a[0]()
+        with torch.cuda.stream(s2):
+            b[0]()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in a[1] + b[1]]
+    for t in a[1] + b[1]:
+        t.zero_()
+    a[0]()
+    b[0]()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, a[1] + b[1]))
+
+
+@pytest.mark.parametrize("prec,R,W,K", [("bf16", 64, 1000, 10), ("fp32", 2, 50001, 20), ("bf16", 4000, 64, 4)])
+def test_graph_replays(prec, R, W, K):
+    """The chain captured into a graph and replayed on changing inputs, with
+    eager work and a synchronisation between the replays."""
+    import torch
+    go, outs, xd = _chain(prec, R, W, K, 3)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        go()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for i in range(4):
+        xd.mul_(-0.75)
+        go()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, outs)), i
