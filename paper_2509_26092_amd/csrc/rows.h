@@ -1,0 +1,85 @@
+// Device helpers of the row operators (layer norm, top logits, distillation):
+// 16-byte chunks of rows that may start at any element, and reductions over
+// groups of lanes.
+#pragma once
+#include "common.h"
+
+namespace rn18 {
+
+// A 16-byte chunk at any element. Global memory takes 16-byte accesses at any
+// byte address here, so rows need no alignment beyond their element's.
+template <typename T>
+__device__ inline uint4 load_chunk(const T* p) {
+  uint4 q;
+  __builtin_memcpy(&q, p, 16);
+  return q;
+}
+template <typename T>
+__device__ inline void store_chunk(T* p, const uint4& q) {
+  __builtin_memcpy(p, &q, 16);
+}
+
+// Chunk c of a row of W >= VW elements: chunks start VW elements apart, and
+// the last one is moved back to end with the row, where its first `skip`
+// elements belong to the chunk before it. A chunk past the row (c >= nch)
+// covers the row's first elements and owns none of them.
+struct ChunkAt {
+  int start, skip;
+};
+template <int VW>
+__device__ inline ChunkAt chunk_at(int c, int W) {
+  const int b = c * VW;
+  if (b >= W) return {0, VW};
+  const int s = b + VW <= W ? b : W - VW;
+  return {s, b - s};
+}
+// The owned elements of a chunk: all in one access where it owns all.
+template <typename T>
+__device__ inline void store_owned(T* row, ChunkAt a, const float* v) {
+  constexpr int VW = TT<T>::VW;
+  if (a.skip == 0) {
+    store_chunk(row + a.start, pack<T>(v));
+  } else {
+#pragma unroll
+    for (int j = 0; j < VW; ++j)
+      if (j >= a.skip) row[a.start + j] = TT<T>::from_f(v[j]);
+  }
+}
+
+// f over the values of L lanes of a wave (L a power of two up to 64, groups
+// aligned); every lane of the group gets the same bits. Lanes are exchanged
+// at distances 1, 2 (quad permutes), 4, 8 (mirrors of half rows and rows,
+// whose halves hold equal values by then), 16 and 32 (row and half-wave
+// swaps). Every lane of the wave takes part.
+template <int CTRL>
+__device__ inline uint32_t dpp_mov(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int L, typename F>
+__device__ inline float group_red(float v, F f) {
+  auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+  auto flt = [](uint32_t x) { return __builtin_bit_cast(float, x); };
+  if (L >= 2) v = f(v, flt(dpp_mov<0xB1>(bits(v))));
+  if (L >= 4) v = f(v, flt(dpp_mov<0x4E>(bits(v))));
+  if (L >= 8) v = f(v, flt(dpp_mov<0x141>(bits(v))));
+  if (L >= 16) v = f(v, flt(dpp_mov<0x140>(bits(v))));
+  if (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
+    v = f(flt(r[0]), flt(r[1]));
+  }
+  if (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
+    v = f(flt(r[0]), flt(r[1]));
+  }
+  return v;
+}
+template <int L>
+__device__ inline float group_sum(float v) {
+  return group_red<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ inline float group_max(float v) {
+  return group_red<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+}  // namespace rn18
