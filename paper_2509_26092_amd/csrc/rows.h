@@ -19,32 +19,12 @@ __device__ inline void store_chunk(T* p, const uint4& q) {
   __builtin_memcpy(p, &q, 16);
 }
 
-// Chunk c of a row of W >= VW elements: chunks start VW elements apart, and
-// the last one is moved back to end with the row, where its first `skip`
-// elements belong to the chunk before it. A chunk past the row (c >= nch)
-// covers the row's first elements and owns none of them.
-struct ChunkAt {
-  int start, skip;
-};
-template <int VW>
-__device__ inline ChunkAt chunk_at(int c, int W) {
-  const int b = c * VW;
-  if (b >= W) return {0, VW};
-  const int s = b + VW <= W ? b : W - VW;
-  return {s, b - s};
-}
-// The owned elements of a chunk: all in one access where it owns all.
-template <typename T>
-__device__ inline void store_owned(T* row, ChunkAt a, const float* v) {
-  constexpr int VW = TT<T>::VW;
-  if (a.skip == 0) {
-    store_chunk(row + a.start, pack<T>(v));
-  } else {
-#pragma unroll
-    for (int j = 0; j < VW; ++j)
-      if (j >= a.skip) row[a.start + j] = TT<T>::from_f(v[j]);
-  }
-}
+// A row of W elements is W / VW whole chunks and up to VW - 1 further
+// elements, its tail, one to a lane.
+
+// Hides where a chunk came from, so that values unpacked from it before are
+// not kept in registers until they are needed again.
+__device__ inline void opaque(uint4& q) { asm volatile("" : "+v"(q.x), "+v"(q.y), "+v"(q.z), "+v"(q.w)); }
 
 // f over the values of L lanes of a wave (L a power of two up to 64, groups
 // aligned); every lane of the group gets the same bits. Lanes are exchanged
