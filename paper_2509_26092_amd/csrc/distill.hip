@@ -1,5 +1,5 @@
-// A teacher's top logits, and the distillation loss of a student against
-// them with the gradient of the student's logits.
+// The distillation loss of a student against a teacher's top logits, with the
+// gradient of the student's logits.
 #include <math.h>
 
 #include "kernels.h"
@@ -11,53 +11,6 @@ namespace {
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
 int row_grid(long R) { return (int)(R < 65536 ? R : 65536); }
-
-// Order-preserving unsigned key of a float: larger value, larger key; the
-// two zeros share a key and every NaN has the largest one.
-__device__ inline uint32_t order_key(float v) {
-  if (v != v) return 0xfffffffeu;   // above +inf; (key, ~class) stays below the all-ones start
-  const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);   // -0 + 0 = +0
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-
-__device__ inline uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    const uint64_t w = __shfl_xor((unsigned long long)v, o);
-    v = w > v ? w : v;
-  }
-  return v;
-}
-
-// One block per row: K rounds, each the largest (key, ~class) below the
-// previous round's.
-template <typename T>
-__global__ __launch_bounds__(256) void topk_kernel(const T* __restrict__ z, float* __restrict__ vals,
-                                                   int32_t* __restrict__ idx, long R, int C, long ldz, int K) {
-  __shared__ uint64_t sh[4];
-  for (long r = blockIdx.x; r < R; r += gridDim.x) {
-    const T* zr = z + r * ldz;
-    uint64_t last = ~0ull;
-    for (int k = 0; k < K; ++k) {
-      uint64_t best = 0;
-      for (int c = threadIdx.x; c < C; c += 256) {
-        const uint64_t e = (uint64_t)order_key(TT<T>::to_f(zr[c])) << 32 | (uint32_t)~c;
-        if (e < last && e > best) best = e;
-      }
-      best = wave_max(best);
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = best;
-      __syncthreads();
-      for (int w = 0; w < 4; ++w) best = sh[w] > best ? sh[w] : best;
-      last = best;
-      if (threadIdx.x == 0) {
-        const int c = (int)~(uint32_t)best;
-        vals[r * K + k] = TT<T>::to_f(zr[c]);
-        idx[r * K + k] = c;
-      }
-    }
-  }
-}
 
 __device__ inline float block_red(float v, float* sh, bool is_max) {
 #pragma unroll
@@ -197,22 +150,6 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(const float* __restri
 }
 
 }  // namespace
-
-size_t topk_workspace(int prec, long R, int C, int K) {
-  (void)prec; (void)R; (void)C; (void)K;
-  return 0;
-}
-
-int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int C, long ldz, int K, void* ws,
-                hipStream_t s) {
-  (void)ws;
-  if (R <= 0) return 0;
-  return with_prec(prec, [&](auto tag) {
-    using T = decltype(tag);
-    hipLaunchKernelGGL(topk_kernel<T>, dim3(row_grid(R)), dim3(256), 0, s, (const T*)z, vals, idx, R, C, ldz, K);
-    return ok();
-  });
-}
 
 size_t distill_workspace(int prec, long R, int C, int K) {
   (void)prec; (void)R; (void)C; (void)K;
