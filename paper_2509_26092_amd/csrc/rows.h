@@ -14,6 +14,14 @@ __device__ inline uint4 load_chunk(const T* p) {
   __builtin_memcpy(&q, p, 16);
   return q;
 }
+// The same at a byte offset below 2^32, which leaves a row's address, where it
+// is the same for the whole wave, out of the lanes' registers.
+template <typename T>
+__device__ inline uint4 load_chunk_at(const T* row, uint32_t bytes) {
+  uint4 q;
+  __builtin_memcpy(&q, (const T*)((const char*)row + bytes), 16);
+  return q;
+}
 template <typename T>
 __device__ inline void store_chunk(T* p, const uint4& q) {
   __builtin_memcpy(p, &q, 16);

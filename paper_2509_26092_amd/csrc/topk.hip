@@ -14,6 +14,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "rows.h"
@@ -31,46 +32,60 @@ __device__ inline uint32_t order_key(float v) {
   const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);   // -0 + 0 = +0
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-// The value of a key whose bits below the type's are cut to zero.
-template <typename T>
+// The smallest value whose key has these leading bits (the others of k are 0).
 __device__ inline float key_value(uint32_t k) {
-  constexpr uint32_t low = prec_of<T>() == PREC_BF16 ? 0xffffu : prec_of<T>() == PREC_F16 ? 0x1fffu : 0u;
-  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~(k | low));
-}
-template <typename T>
-__device__ constexpr int key_bits() {   // leading bits of a key that tell values of the type apart
-  return prec_of<T>() == PREC_BF16 ? 16 : prec_of<T>() == PREC_F16 ? 19 : 32;
+  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// max(a, b, c) in one instruction. A NaN may drop out with what it meets:
-// the result is a number of the row or a NaN.
+// The largest of a, b and c, or a NaN if one of them is (one instruction).
 __device__ inline float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
+template <int VW>
+__device__ inline float chunk_max(const float* v) {
+  float m = max3(v[0], v[1], v[2]);
+#pragma unroll
+  for (int j = 3; j + 1 < VW; j += 2) m = max3(m, v[j], v[j + 1]);
+  return __builtin_elementwise_maximum(m, v[VW - 1]);
+}
+// The key of a maximum that a bound may rest on: 0 for a NaN's.
+__device__ inline uint32_t max_key(float m) { return m == m ? order_key(m) : 0; }
 
-// The K-th largest of the 64 * PER keys that a wave holds, cut to `bits`
-// leading bits; 0 if there are fewer.
-template <int PER>
-__device__ inline uint32_t kth_key(const uint32_t (&k)[PER], int K, int bits) {
-  uint32_t t = 0;
-  for (int b = 31; b >= 32 - bits; --b) {
-    const uint32_t c = t | 1u << b;
+// A bound for the K-th largest of the 64 * PER keys that a wave holds: its
+// leading kBoundBits bits (sign, exponent and 5 bits of the mantissa: it is
+// less than 1/32 below, which adds a few entries to the list and takes a
+// third of the steps of 32 bits off); 0 if there are fewer than K keys.
+constexpr int kBoundBits = 14;
+template <int PER, typename F>
+__device__ inline uint32_t kth_key(F key, int K) {   // key(p): the lane's p-th
+  auto enough = [&](uint32_t c) {
     int n = 0;
 #pragma unroll
-    for (int p = 0; p < PER; ++p) n += __popcll(__ballot(k[p] >= c));
-    if (n >= K) t = c;
+    for (int p = 0; p < PER; ++p) n += __popcll(__ballot(key(p) >= c));
+    return n >= K;
+  };
+  // from 2 to 2^32, with the sign: where the K-th logit of most rows lies
+  uint32_t t = 0xc0000000u;
+  int b = 28;
+  if (!enough(t) || enough(0xd0000000u)) {
+    t = 0;
+    b = 31;
+  }
+#pragma unroll 1
+  for (; b >= 32 - kBoundBits; --b) {
+    const uint32_t c = t | 1u << b;
+    if (enough(c)) t = c;
   }
   return t;
 }
 
 template <int L>
 struct TopShared {
-  static constexpr int M = L > 64 ? 2048 : 256;   // entries of the list
+  static constexpr int M = L > 512 ? 2048 : L > 64 ? 1024 : 256;   // entries of the list
   uint64_t list[M];
-  uint32_t keys[L];
-  uint32_t count, bound;
+  uint32_t chunk[M];
+  uint32_t keys[L > 64 ? L : 1];
+  uint32_t count, chunks, bound;
   int part[16];
 };
 
@@ -86,102 +101,100 @@ __device__ inline void row_sync() {
   }
 }
 
-// Sum over the row's lanes, and the sum over the lanes before this one.
+// Sum over the row's waves of a count that each holds, and the sum over the
+// waves before this one.
 template <int L>
 __device__ inline int row_count(int n, int* before, TopShared<L>& sh) {
-  const int lane = threadIdx.x & 63;
-  int inc = n;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(inc, o);
-    if (lane >= o) inc += up;
+  *before = 0;
+  if (L == 64) return n;
+  const int w = threadIdx.x >> 6;
+  __syncthreads();   // earlier readers of part are done
+  if ((threadIdx.x & 63) == 0) sh.part[w] = n;
+  __syncthreads();
+  int total = 0;
+  for (int i = 0; i < L / 64; ++i) {
+    if (i < w) *before += sh.part[i];
+    total += sh.part[i];
   }
-  int base = 0, total = __shfl(inc, 63);
-  if (L > 64) {
-    const int w = threadIdx.x >> 6;
-    __syncthreads();   // earlier readers of part are done
-    if (lane == 63) sh.part[w] = inc;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < L / 64; ++i) {
-      if (i < w) base += sh.part[i];
-      total += sh.part[i];
-    }
-  }
-  *before = base + inc - n;
   return total;
 }
 
-// REG: a row is E chunks a lane and its tail, kept in registers; otherwise it
-// is read again from memory in every phase.
+// REG: a lane has E chunks, whose maxima it keeps; otherwise any number, and
+// it reads them again to find those that reach the bound. A row may be cut into gridDim.y
+// parts of `len` logits, whose entries (key, ~class) go to
+// part[row][part][K].
 template <typename T, int L, int E, bool REG>
 __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __restrict__ z, float* __restrict__ vals,
-                                                                 int32_t* __restrict__ idx, long R, int C, long ldz,
-                                                                 int K) {
+                                                                 int32_t* __restrict__ idx,
+                                                                 uint64_t* __restrict__ part, long R, int Call, int len,
+                                                                 long ldz, int K) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L;
   constexpr int M = TopShared<L>::M;
   __shared__ TopShared<L> shared[G];
   TopShared<L>& sh = shared[L < NT ? threadIdx.x / L : 0];
-  const int nch = C / VW, steps = (nch + L - 1) / L;
-  for (long b = (long)blockIdx.x * G; b < R; b += (long)gridDim.x * G) {
+  const int first = (int)blockIdx.y * len;
+  const int C = std::min(len, Call - first);
+  // (L < NT: each wave has its own rows, and nothing waits for another's)
+  for (long r = (long)blockIdx.x * G + (L < NT ? threadIdx.x / L : 0); r < R; r += (long)gridDim.x * G) {
     int l = threadIdx.x % L;
     asm volatile("" : "+v"(l));   // classes are computed where they are needed, not kept over the rows
-    const int tail = nch * VW + l;
-    const long r = b + (L < NT ? threadIdx.x / L : 0);
-    if (L < NT && r >= R) return;   // whole waves, which nothing waits for
-    const T* zr = z + r * ldz;
-    uint4 q[REG ? E : 1];
-    T qt{};
-    if (REG) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) q[e] = load_chunk(zr + (e * L + l < nch ? (e * L + l) * VW : 0));
-    }
-    if (tail < C) qt = zr[tail];
-    // f(values, first class) over the lane's chunks: from memory, and from the
-    // registers if they are there
-    auto chunks_again = [&](auto f) {
-      float v[VW];
-#pragma unroll 1
-      for (int c = l; c < nch; c += L) {
-        unpack<T>(load_chunk(zr + (long)c * VW), v);
-        f(v, c * VW);
-      }
-    };
-    auto chunks = [&](auto f) {
-      if constexpr (REG) {
-        float v[VW];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e * L + l < nch) {
-            unpack<T>(q[e], v);
-            f(v, (e * L + l) * VW);
-            opaque(q[e]);
-            __builtin_amdgcn_sched_barrier(0);   // one chunk's values at a time in registers
-          }
-      } else {
-        chunks_again(f);
-      }
-    };
-    float top = tail < C ? TT<T>::to_f(qt) : -INFINITY;
-    chunks([&](const float* v, int) {
-#pragma unroll
-      for (int j = 0; j < VW; j += 2) top = max3(top, v[j], v[j + 1]);
-    });
-    if (!(top == top)) top = -INFINITY;   // any number that no logit of the lane is below is a bound
+    const T* zr = z + r * ldz + first;
+    // Chunks start at the row's first 16-byte boundary (at odd ones a row of
+    // 131071 fp16 logits took 12.3 us in place of 8.1); the up to VW - 1
+    // logits before it and after the last chunk are one to a lane.
+    const int head = std::min(C, (int)((0 - (uintptr_t)zr) & 15) / (int)sizeof(T));
+    const int nch = (C - head) / VW;
+    const T* zc = zr + head;
+    const int tail = l < head ? l : nch * VW + l;
+    const float vt = TT<T>::to_f(zr[tail < C ? tail : 0]);
 
-    // the bound: the K-th largest of the lanes' maxima, or of those of fours
-    // of lanes where these are enough
-    const int bits = key_bits<T>();
-    float bound;
+    // the bound: the K-th largest of the maxima of chunks (of a wave's row),
+    // lanes, or fours of lanes where these are enough
+    uint32_t kth;
+    float tops[REG ? E : 1];   // the largest of each of the lane's chunks
+    if (l == 0) sh.count = sh.chunks = 0;
+    if constexpr (REG) {
+      constexpr int B = E < 8 ? E : 8;   // chunks in flight
+#pragma unroll
+      for (int e0 = 0; e0 < E; e0 += B) {
+        uint4 q[B] = {};
+        if (nch > 0) {
+#pragma unroll
+          for (int e = 0; e < B; ++e) {
+            const int c = (e0 + e) * L + l;
+            q[e] = load_chunk_at(zc, (c < nch ? c : 0) * 16u);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < B; ++e) {
+          float v[VW];
+          unpack<T>(q[e], v);
+          tops[e0 + e] = (e0 + e) * L + l < nch ? chunk_max<VW>(v) : -INFINITY;
+        }
+        if (e0 + B < E) __builtin_amdgcn_sched_barrier(0);   // registers for B chunks, so that two blocks fit a compute unit
+      }
+    }
     if constexpr (L == 64) {
-      const uint32_t k[1] = {order_key(top)};
-      bound = key_value<T>(kth_key<1>(k, K, bits));
+      uint32_t k[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) k[e] = max_key(tops[e]);
+      kth = kth_key<E>([&](int p) { return k[p]; }, K);
     } else {
-      const bool fours = K * 16 <= L;
+      float top = tail < C ? vt : -INFINITY;
+      if constexpr (REG) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = __builtin_elementwise_maximum(top, tops[e]);
+      } else {
+        float v[VW];
+        for (int c = l; c < nch; c += L) {
+          unpack<T>(load_chunk(zc + (long)c * VW), v);
+          top = __builtin_elementwise_maximum(top, chunk_max<VW>(v));
+        }
+      }
+      const bool fours = K * 8 <= L;
+      if (!(top == top)) top = -INFINITY;
       if (fours) top = group_max<4>(top);
-      if (!fours || (l & 3) == 0) sh.keys[fours ? l >> 2 : l] = order_key(top);
-      if (l == 0) sh.count = 0;
+      if (!fours || (l & 3) == 0) sh.keys[fours ? l >> 2 : l] = max_key(top);
       __syncthreads();
       if (threadIdx.x < 64) {
         uint32_t t;
@@ -189,54 +202,77 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
           uint32_t k[L / 256];
 #pragma unroll
           for (int p = 0; p < L / 256; ++p) k[p] = sh.keys[p * 64 + l];
-          t = kth_key<L / 256>(k, K, bits);
+          t = kth_key<L / 256>([&](int p) { return k[p]; }, K);
         } else {
-          uint32_t k[L / 64];
+          // (registers for four keys, no more: a block's other waves need none)
+          uint32_t k[4];
 #pragma unroll
-          for (int p = 0; p < L / 64; ++p) k[p] = sh.keys[p * 64 + l];
-          t = kth_key<L / 64>(k, K, bits);
+          for (int p = 0; p < 4; ++p) k[p] = sh.keys[p * 64 + l];
+          t = kth_key<L / 64>([&](int p) { return p < 4 ? k[p] : sh.keys[p * 64 + l]; }, K);
         }
         if (l == 0) sh.bound = t;
       }
       __syncthreads();
-      bound = key_value<T>(sh.bound);
+      kth = sh.bound;
     }
-    if (L == 64) {
-      if (l == 0) sh.count = 0;
-      row_sync<L>();
-    }
-    if (!(bound == bound)) bound = -INFINITY;   // no key: fewer lanes than K
+    float bound = key_value(kth);
+    if (!(bound == bound)) bound = -INFINITY;   // fewer maxima than K, or cut to below the key of -inf
 
+    // The chunks whose maximum reaches the bound (a NaN does), then, a lane for
+    // each of their logits, the list of those that do, in any order. (Few
+    // lanes of a wave have such a chunk, so the lanes would idle if each went
+    // through its own.)
+    if (L == 64) row_sync<L>();   // (the counts are zero)
+    if constexpr (REG) {
+      uint32_t hit = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) hit |= !(tops[e] < bound) && e * L + l < nch ? 1u << e : 0u;
+      if (hit) {
+        uint32_t at = atomicAdd(&sh.chunks, (uint32_t)__popc(hit));
+#pragma unroll 1
+        for (; hit; hit &= hit - 1, ++at)
+          if (at < M) sh.chunk[at] = (uint32_t)((__ffs(hit) - 1) * L + l);
+      }
+    } else {
+      for (int c = l; c < nch; c += L) {
+        float v[VW];
+        unpack<T>(load_chunk(zc + (long)c * VW), v);
+        if (!(chunk_max<VW>(v) < bound)) {
+          const uint32_t at = atomicAdd(&sh.chunks, 1u);
+          if (at < M) sh.chunk[at] = (uint32_t)c;
+        }
+      }
+    }
     auto take = [&](float v, int c) {
       const uint32_t at = atomicAdd(&sh.count, 1u);
       if (at < M) sh.list[at] = (uint64_t)order_key(v) << 32 | (uint32_t)~c;
     };
-    chunks([&](const float* v, int c) {
-      bool some = false;
-#pragma unroll
-      for (int j = 0; j < VW; ++j) some |= !(v[j] < bound);
-      if (some) {
-#pragma unroll
-        for (int j = 0; j < VW; ++j)
-          if (!(v[j] < bound)) take(v[j], c + j);
-      }
-    });
-    if (tail < C && !(TT<T>::to_f(qt) < bound)) take(TT<T>::to_f(qt), tail);
+    if (tail < C && !(vt < bound)) take(vt, tail);
     row_sync<L>();
-    int n = (int)sh.count;
+    const int hits = (int)sh.chunks;
+    if (hits <= M)
+#pragma unroll 1
+      for (int i = l; i < hits * VW; i += L) {
+        const int c = head + (int)sh.chunk[i / VW] * VW + i % VW;
+        const float v = TT<T>::to_f(zr[c]);
+        if (!(v < bound)) take(v, c);
+      }
+    row_sync<L>();
+    int n = hits <= M ? (int)sh.count : M + 1;
     if (n > M) {
-      // count of logits above a key
-      auto above = [&](uint32_t k) {
-        int s = tail < C && order_key(TT<T>::to_f(qt)) > k ? 1 : 0, before;
-        chunks_again([&](const float* v, int) {
-#pragma unroll
-          for (int j = 0; j < VW; ++j) s += order_key(v[j]) > k ? 1 : 0;
-        });
+      // (one logit at a time: few rows come here, and the registers of the
+      // common path set how many rows are in flight)
+      auto above = [&](uint32_t k) {   // count of logits above a key
+        int s = 0, before;
+#pragma unroll 4
+        for (int c = l; c - l < C; c += L)
+          s += __popcll(__ballot(c < C && order_key(TT<T>::to_f(zr[c < C ? c : 0])) > k));
         return row_count<L>(s, &before, sh);
       };
       // above(lo) > M, above(hi) < K; the bound's own key is the likely answer
       uint32_t lo = order_key(bound) - 1, hi = 0xffffffffu, at = lo + 1;
       int have = 0;
+#pragma unroll 1
       while (hi - lo > 1) {
         have = above(at);
         if (have > M) lo = at;
@@ -251,37 +287,19 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
       row_sync<L>();
       if (l == 0) sh.count = 0;
       row_sync<L>();
-      auto take_above = [&](float v, int c) {
-        if (order_key(v) > at) take(v, c);
-      };
-      chunks_again([&](const float* v, int c) {
-#pragma unroll
-        for (int j = 0; j < VW; ++j) take_above(v[j], c + j);
-      });
-      if (tail < C) take_above(TT<T>::to_f(qt), tail);
+#pragma unroll 1
+      for (int c = l; c < C; c += L)
+        if (const float v = TT<T>::to_f(zr[c]); order_key(v) > at) take(v, c);
       n = have;
-      for (int e = 0; e <= steps && n < K; ++e) {   // e = steps: the tail
-        float v[VW];
-        const int c = e * L + l;
-        int first = c * VW, count = c < nch ? VW : 0;
-        if (e == steps) {
-          first = tail;
-          count = tail < C ? 1 : 0;
-          v[0] = TT<T>::to_f(qt);
-        } else if (count) {
-          unpack<T>(load_chunk(zr + first), v);
-        }
-        int same = 0, before;
-#pragma unroll
-        for (int j = 0; j < VW; ++j) same += j < count && order_key(v[j]) == at ? 1 : 0;
-        const int total = row_count<L>(same, &before, sh);
-        before += n;
-#pragma unroll
-        for (int j = 0; j < VW; ++j)
-          if (j < count && order_key(v[j]) == at) {
-            if (before < K) sh.list[before] = (uint64_t)at << 32 | (uint32_t)~(first + j);
-            ++before;
-          }
+#pragma unroll 1
+      for (int c0 = 0; c0 < C && n < K; c0 += L) {
+        const int c = c0 + l;
+        const bool same = c < C && order_key(TT<T>::to_f(zr[c < C ? c : 0])) == at;
+        const uint64_t who = __ballot(same);
+        int before;
+        const int total = row_count<L>(__popcll(who), &before, sh);
+        before += n + __popcll(who & ((1ull << (threadIdx.x & 63)) - 1));
+        if (same && before < K) sh.list[before] = (uint64_t)at << 32 | (uint32_t)~c;
         n = std::min(K, n + total);
       }
       row_sync<L>();
@@ -290,58 +308,127 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
     int per = 1;
     while (per < 16 && n * per * 2 <= L) per *= 2;
     const int sub = l & (per - 1);
+#pragma unroll 1
     for (int i0 = 0; i0 < n; i0 += L / per) {
       const int i = i0 + l / per;
       const uint64_t mine = i < n ? sh.list[i] : ~0ull;
       int place = 0;
+#pragma unroll 4
       for (int j = sub; j < n; j += per) place += sh.list[j] > mine ? 1 : 0;
       for (int o = 1; o < per; o <<= 1) place += __shfl_xor(place, o);
       if (i < n && sub == 0 && place < K) {
         const int c = (int)~(uint32_t)mine;
-        vals[r * K + place] = TT<T>::to_f(zr[c]);
-        idx[r * K + place] = c;
+        if (gridDim.y > 1) {
+          part[(r * gridDim.y + blockIdx.y) * K + place] = mine - first;   // ~(c + first)
+        } else {
+          vals[r * K + place] = TT<T>::to_f(zr[c]);
+          idx[r * K + place] = c;
+        }
       }
     }
     row_sync<L>();   // before the next row's list
   }
 }
 
+// The places of a row's n entries from all its parts: 8 lanes count for each.
+constexpr int kMergeMax = 2048;
+template <typename T>
+__global__ __launch_bounds__(1024) void topk_merge_kernel(const T* __restrict__ z, float* __restrict__ vals,
+                                                          int32_t* __restrict__ idx, const uint64_t* __restrict__ part,
+                                                          long R, long ldz, int K, int n) {
+  __shared__ uint64_t list[kMergeMax];
+  const int sub = threadIdx.x & 7;
+  for (long r = blockIdx.x; r < R; r += gridDim.x) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 1024) list[i] = part[r * n + i];
+    __syncthreads();
+    for (int i0 = 0; i0 < n; i0 += 128) {
+      const int i = i0 + (int)(threadIdx.x >> 3);
+      const uint64_t mine = i < n ? list[i] : ~0ull;
+      int place = 0;
+#pragma unroll 8
+      for (int j = sub; j < n; j += 8) place += list[j] > mine ? 1 : 0;
+      for (int o = 1; o < 8; o <<= 1) place += __shfl_xor(place, o);
+      if (i < n && sub == 0 && place < K) {
+        const int c = (int)~(uint32_t)mine;
+        vals[r * K + place] = TT<T>::to_f(z[r * ldz + c]);
+        idx[r * K + place] = c;
+      }
+    }
+  }
+}
+
+struct TopPlan {
+  int parts, len;
+};
+// Rows of more than 2^14 chunks, more than a block keeps the maxima of, are
+// cut into parts of up to 2^13 (512 rows of 131071 fp32 logits: 58 us; in
+// parts of 2^14, of which a compute unit holds one at a time, 69 us; fewer
+// rows or shorter ones gain nothing from parts: the launch that joins them
+// costs what they save).
+TopPlan topk_plan(int prec, int C, int K) {
+  const int vw = prec_vw(prec);
+  if (C / vw <= 16384) return {1, C};
+  const int most = 8192 * vw;
+  const int parts = ceil_div(C, most);
+  const int len = (ceil_div(C, parts) + vw - 1) / vw * vw;
+  // (the last part is the shortest and still holds K)
+  if ((long)parts * K > kMergeMax || (long)(parts - 1) * len + K > C) return {1, C};
+  return {parts, len};
+}
+
 template <typename T, int L, int E, bool REG = true, typename... A>
-int topk_go(long R, hipStream_t s, A... a) {
+int topk_go(long R, int parts, hipStream_t s, A... a) {
   constexpr int NT = L > 256 ? L : 256, G = NT / L;
-  const long units = (R + G - 1) / G;
-  hipLaunchKernelGGL((topk_kernel<T, L, E, REG>), dim3((unsigned)std::min(units, 1l << 20)), dim3(NT), 0, s, a...);
+  const long units = std::min((R + G - 1) / G, 1l << 22);
+  hipLaunchKernelGGL((topk_kernel<T, L, E, REG>), dim3((unsigned)units, parts), dim3(NT), 0, s, a...);
   return ok();
 }
 
 }  // namespace
 
 size_t topk_workspace(int prec, long R, int C, int K) {
-  (void)prec; (void)R; (void)C; (void)K;
-  return 0;
+  const TopPlan pl = topk_plan(prec, C, K);
+  return pl.parts > 1 && R > 0 ? (size_t)R * pl.parts * K * 8 : 0;
 }
 
 int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int C, long ldz, int K, void* ws,
                 hipStream_t s) {
-  (void)ws;
   if (R <= 0) return 0;
+  const TopPlan pl = topk_plan(prec, C, K);
   return with_prec(prec, [&](auto tag) {
     using T = decltype(tag);
     const T* zt = (const T*)z;
-    const int nch = C / TT<T>::VW;
-    if (K <= 16 && nch <= 256) {
-      if (nch <= 64) return topk_go<T, 64, 1>(R, s, zt, vals, idx, R, C, ldz, K);
-      if (nch <= 128) return topk_go<T, 64, 2>(R, s, zt, vals, idx, R, C, ldz, K);
-      return topk_go<T, 64, 4>(R, s, zt, vals, idx, R, C, ldz, K);
-    }
-    if (nch <= 256) return topk_go<T, 256, 1>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 512) return topk_go<T, 256, 2>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 1024) return topk_go<T, 256, 4>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 2048) return topk_go<T, 256, 8>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 4096) return topk_go<T, 512, 8>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 8192) return topk_go<T, 1024, 8>(R, s, zt, vals, idx, R, C, ldz, K);
-    if (nch <= 16384) return topk_go<T, 1024, 16>(R, s, zt, vals, idx, R, C, ldz, K);
-    return topk_go<T, 1024, 1, false>(R, s, zt, vals, idx, R, C, ldz, K);
+    uint64_t* part = (uint64_t*)ws;
+    const int nch = pl.len / TT<T>::VW;
+    auto go = [&](auto l, auto e, auto reg) {
+      return topk_go<T, decltype(l)::value, decltype(e)::value, decltype(reg)::value>(R, pl.parts, s, zt, vals, idx, part,
+                                                                                     R, C, pl.len, ldz, K);
+    };
+    auto pick = [&]() {
+#define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{}, std::true_type{})
+      // a wave per row where its chunks are several times K or its logits fit the list
+      if (K <= 64 && nch <= 512 && (nch * 2 >= K * 3 || pl.len <= TopShared<64>::M)) {
+        if (nch <= 64) GO(64, 1);
+        if (nch <= 128) GO(64, 2);
+        if (nch <= 256) GO(64, 4);
+        GO(64, 8);
+      }
+      if (nch <= 256) GO(256, 1);
+      if (nch <= 512) GO(256, 2);
+      if (nch <= 1024) GO(256, 4);
+      if (nch <= 2048) GO(256, 8);
+      if (nch <= 4096) GO(512, 8);
+      if (nch <= 8192) GO(512, 16);
+      if (nch <= 16384) GO(1024, 16);
+#undef GO
+      return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{}, std::false_type{});
+    };
+    int r = pick();
+    if (r || pl.parts == 1) return r;
+    hipLaunchKernelGGL(topk_merge_kernel<T>, dim3((unsigned)std::min(R, 1l << 22)), dim3(1024), 0, s, zt, vals, idx,
+                       (const uint64_t*)part, R, ldz, K, pl.parts * K);
+    return ok();
   });
 }
 
