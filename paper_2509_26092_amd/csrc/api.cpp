@@ -1840,7 +1840,7 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
   if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
   if ((r = ws_check(ws, ws_bytes, distill_workspace(prec, R, C, K)))) return r;
   const DistillArgs a{z, t_vals, t_idx, labels, row_weight, dz, row_loss, R, ldz, lddz, C, K, temperature, alpha,
-                      scale};
+                      scale, nullptr, nullptr};
   LCHK(distill_launch(prec, a, loss, ws, (hipStream_t)stream));
   return RN18_OK;
 }

@@ -1,8 +1,24 @@
 // The distillation loss of a student against a teacher's top logits, with the
-// gradient of the student's logits.
+// gradient of the student's logits:
+//   P = softmax(z / T), p = softmax(z), q = softmax of the teacher's valid
+//   entries t / T
+//   row_loss = w (alpha T^2 sum_k q_k (log q_k - log P_{i_k}) + (1 - alpha) (-log p_label))
+//   dz_j = scale w (alpha T (P_j - sum_{k: i_k = j} q_k) + (1 - alpha) (p_j - [j = label]))
+//
+// z is read once into registers, its maximum and sums of exponentials are
+// taken there, and dz is written from there: 4 bytes of traffic and two or
+// four exponentials an element in 16 bits. The few classes that the list or the
+// label name are written a second time with their own terms, by the lane of
+// the first entry that names each. With sum q = 1 the soft term is
+// sum_k q_k (t'_k - z'_k) - log sum e^t' + log sum e^z' (t', z': over T, less
+// their maxima), so that every sum of a row is taken in one step.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "kernels.h"
+#include "rows.h"
 
 namespace rn18 {
 
@@ -10,160 +26,432 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
-int row_grid(long R) { return (int)(R < 65536 ? R : 65536); }
+constexpr float kLog2e = 1.44269504088896340736f;
+// 2^x by the hardware's instruction (1 ulp; 0 below 2^-126)
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ inline float block_red(float v, float* sh, bool is_max) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    const float w = __shfl_xor(v, o);
-    v = is_max ? fmaxf(v, w) : v + w;
+// The teacher's list of a row and, as entry K, the label.
+struct Entries {
+  int32_t cls[kTopMax + 1];   // -1: not valid
+  float e[kTopMax + 1];       // t / T, then exp(t / T - their maximum)
+  float z[kTopMax + 1];       // the student's logit
+};
+
+// Loads a row's entries; zk: the student's logits of the entries, if they
+// have been gathered before, or NULL. Returns the largest t / T.
+template <typename T, int L, bool HARD>
+__device__ inline float load_entries(const DistillArgs& a, long r, int l, const T* zr, const float* zk, Entries& en) {
+  const float invt = 1.0f / a.temperature;
+  float tm = -INFINITY;
+  bool bad = false;
+  for (int k = l; k <= a.K; k += L) {
+    float t = -INFINITY;
+    int i = -1;
+    if (k < a.K) {
+      i = a.t_idx[r * a.K + k];
+      t = a.t_vals[r * a.K + k] * invt;
+      bad |= i < -1 || i >= a.C;
+      if (i < 0 || i >= a.C || t == -INFINITY) {
+        i = -1;
+        t = -INFINITY;
+      }
+    } else if (HARD) {
+      i = a.labels[r];
+      if (i < 0 || i >= a.C) {
+        bad = true;
+        i = -1;
+      }
+    }
+    en.cls[k] = i;
+    en.e[k] = t;
+    en.z[k] = i < 0 ? 0.f : zk ? zk[k] : TT<T>::to_f(zr[i]);
+    tm = max2(tm, t);
   }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  if (is_max) return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+  if (a.err && bad) atomicOr(a.err, (unsigned)DEVERR_LABEL);
+  return tm;
 }
 
-// One block per row, three passes over it: maximum, sums of exponentials,
-// gradient. The classes that the teacher's list or the label name are
-// written last, by the thread of the first list entry that names them.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_kernel(DistillArgs a) {
-  __shared__ float sh[4];
-  __shared__ float q[kTopMax], tv[kTopMax];
-  __shared__ int32_t qi[kTopMax];
-  const T* z = (const T*)a.z;
-  T* dz = (T*)a.dz;
+// A row's sums: of exp(z') and exp(z - m) over the classes, of e and of
+// e (t' - z') over the entries.
+enum { SUM_T, SUM_1, SUM_Q, SUM_QD, SUMS };
+
+template <int L>
+__device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, Entries& en, float* s) {
   const float invt = 1.0f / a.temperature;
-  for (long r = blockIdx.x; r < a.R; r += gridDim.x) {
-    const T* zr = z + r * a.ldz;
-    T* dr = dz ? dz + r * a.lddz : nullptr;
+  for (int k = l; k < a.K; k += L) {
+    const float t = en.e[k] - tm, e = en.cls[k] < 0 ? 0.f : exp2_hw(t * kLog2e);
+    en.e[k] = e;
+    s[SUM_Q] += e;
+    if (e != 0.f) s[SUM_QD] += e * (t - (en.z[k] - m) * invt);
+  }
+  if (l == 0) en.e[a.K] = 0.f;
+}
+
+// What the gradient of a row needs: dz_j = exp(z') gt + exp(z - m) g1, less
+// ft q and fh at the entries and the label.
+struct RowGrad {
+  float m, ct, gt, g1, fq, fh;
+};
+template <bool HARD>
+__device__ inline RowGrad row_grad(const DistillArgs& a, float w, float m, const float* s, bool labelled) {
+  const bool some = s[SUM_T] != 0.f;   // false: every class of the row is masked
+  const bool soft = some && s[SUM_Q] != 0.f, hard = HARD && some && labelled;
+  const float f = a.scale * w * (a.ls ? a.ls->scale : 1.0f);
+  const float ft = f * a.alpha * a.temperature, fh = f * (1.0f - a.alpha);
+  RowGrad g;
+  g.m = m;
+  g.ct = kLog2e / a.temperature;
+  g.gt = soft ? ft / s[SUM_T] : 0.f;
+  g.fq = soft ? ft / s[SUM_Q] : 0.f;
+  g.g1 = hard ? fh / s[SUM_1] : 0.f;
+  g.fh = hard ? fh : 0.f;
+  return g;
+}
+template <bool HARD>
+__device__ inline float grad_at(const RowGrad& g, float z) {
+  const float d = z - g.m;
+  float v = exp2_hw(d * g.ct) * g.gt;
+  if (HARD) v += exp2_hw(d * kLog2e) * g.g1;
+  return v;
+}
+template <bool HARD>
+__device__ inline float row_loss_of(const DistillArgs& a, float w, const float* s, float m, float zlab, bool labelled) {
+  const bool some = s[SUM_T] != 0.f;
+  float v = 0.f;
+  if (some && s[SUM_Q] != 0.f)
+    v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] - logf(s[SUM_Q]) + logf(s[SUM_T]));
+  if (HARD && some && labelled) v += (1.0f - a.alpha) * (logf(s[SUM_1]) - (zlab - m));
+  return w * v;
+}
+
+// The gradients of the classes [c0, c1) that entries name, each by the lane
+// of the first entry that names it.
+template <typename T, int L, bool HARD>
+__device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries& en, T* dr, int c0,
+                                     int c1) {
+  for (int k = l; k <= a.K; k += L) {
+    const int at = en.cls[k];
+    if (at < c0 || at >= c1) continue;
+    bool first = true;
+    float q = 0.f;
+    for (int j = 0; j < a.K; ++j)
+      if (en.cls[j] == at) {
+        first &= j >= k;
+        q += en.e[j];
+      }
+    if (!first) continue;
+    float v = grad_at<HARD>(g, en.z[k]) - g.fq * q;
+    if (HARD && at == en.cls[a.K]) v -= g.fh;
+    dr[at] = TT<T>::from_f(v);
+  }
+}
+
+// One row in the registers of L lanes, E chunks each and a tail.
+template <typename T, int L, int E, bool HARD>
+__global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillArgs a) {
+  constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L;
+  __shared__ Entries entries[G];
+  __shared__ float shm[L > 64 ? L / 64 : 1][2], shs[L > 64 ? L / 64 : 1][SUMS];
+  const int grp = L < NT ? threadIdx.x / L : 0;
+  Entries& en = entries[grp];
+  const int nch = a.C / VW;
+  // (L < NT: each wave has its own rows, and nothing waits for another's)
+  for (long r = (long)blockIdx.x * G + grp; r < a.R; r += (long)gridDim.x * G) {
+    int l = threadIdx.x % L;
+    asm volatile("" : "+v"(l));   // offsets are computed where they are needed, not kept over the rows
+    const T* zr = (const T*)a.z + r * a.ldz;
+    T* dr = a.dz ? (T*)a.dz + r * a.lddz : nullptr;
+    const int tail = nch * VW + l;
     const float w = a.weight ? a.weight[r] : 1.0f;
-    if (w == 0.f) {
-      for (int c = threadIdx.x; dr && c < a.C; c += 256) dr[c] = TT<T>::from_f(0.f);
-      if (threadIdx.x == 0) a.row_loss[r] = 0.f;
+    if (w == 0.f) {   // the row may hold anything: not read
+      if (l == 0) a.row_loss[r] = 0.f;
+      if (dr) {
+        for (int c = l; c < nch; c += L) store_chunk(dr + c * VW, make_uint4(0, 0, 0, 0));
+        if (tail < a.C) dr[tail] = TT<T>::from_f(0.f);
+      }
       continue;
     }
-    const int lab = a.labels && a.alpha != 1.0f ? a.labels[r] : -1;
-    const bool hard = lab >= 0 && lab < a.C;
-    // the teacher's distribution over its valid entries
-    float tm = -INFINITY;
-    __syncthreads();
-    for (int k = threadIdx.x; k < a.K; k += 256) {
-      const int i = a.t_idx[r * a.K + k];
-      const float t = a.t_vals[r * a.K + k] * invt;
-      const bool valid = i >= 0 && i < a.C && t != -INFINITY;
-      qi[k] = valid ? i : -1;
-      tv[k] = valid ? t : -INFINITY;
-      if (valid) tm = fmaxf(tm, t);
+    uint4 q[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      q[e] = nch ? load_chunk_at(zr, (e * L + l < nch ? e * L + l : 0) * 16u) : make_uint4(0, 0, 0, 0);
+    const float zt = tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
+    float mx[2] = {zt, load_entries<T, L, HARD>(a, r, l, zr, nullptr, en)};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float v[VW];
+      unpack<T>(q[e], v);
+      if (e * L + l < nch) mx[0] = max2(mx[0], chunk_max<VW>(v));
+      opaque(q[e]);
+      __builtin_amdgcn_sched_barrier(0);   // one chunk's values at a time in registers
     }
-    tm = block_red(tm, sh, true);
-    if (tm == -INFINITY) tm = 0.f;
-    float ts = 0.f;
-    for (int k = threadIdx.x; k < a.K; k += 256) {
-      q[k] = qi[k] < 0 ? 0.f : expf(tv[k] - tm);
-      ts += q[k];
-    }
-    ts = block_red(ts, sh, false);
-    float m = -INFINITY;
-    for (int c = threadIdx.x; c < a.C; c += 256) m = fmaxf(m, TT<T>::to_f(zr[c]));
-    m = block_red(m, sh, true);
-    if (m == -INFINITY) m = 0.f;
-    float s1 = 0.f, st = 0.f;
-    for (int c = threadIdx.x; c < a.C; c += 256) {
-      const float d = TT<T>::to_f(zr[c]) - m;
-      s1 += expf(d);
-      st += expf(d * invt);
-    }
-    s1 = block_red(s1, sh, false);
-    st = block_red(st, sh, false);
-    const bool some = st != 0.f;              // false: every class of the row is masked
-    const bool soft_on = ts != 0.f && some, hard_on = hard && some;
-    const float lse_t = logf(st), lse_q = logf(ts);
-    float l = 0.f;
-    if (soft_on)
-      for (int k = threadIdx.x; k < a.K; k += 256) {
-        const float p = q[k] / ts;
-        if (qi[k] >= 0 && p != 0.f)
-          l += p * ((tv[k] - tm - lse_q) - ((TT<T>::to_f(zr[qi[k]]) - m) * invt - lse_t));
+    row_red<L>(mx, shm, Max());
+    const float m = mx[0] == -INFINITY ? 0.f : mx[0], tm = mx[1] == -INFINITY ? 0.f : mx[1];
+    const float ct = kLog2e / a.temperature;
+    float s[SUMS] = {exp2_hw((zt - m) * ct), HARD ? exp2_hw((zt - m) * kLog2e) : 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float v[VW];
+      unpack<T>(q[e], v);
+      if (e * L + l < nch) {
+#pragma unroll
+        for (int j = 0; j < VW; ++j) {
+          const float d = v[j] - m;
+          s[SUM_T] += exp2_hw(d * ct);
+          if (HARD) s[SUM_1] += exp2_hw(d * kLog2e);
+        }
       }
-    l = block_red(l, sh, false);
-    if (threadIdx.x == 0) {
-      float v = soft_on ? a.alpha * a.temperature * a.temperature * l : 0.f;
-      if (hard_on) v += (1.0f - a.alpha) * (logf(s1) - (TT<T>::to_f(zr[lab]) - m));
-      a.row_loss[r] = w * v;
+      opaque(q[e]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (L == 64) row_sync<L>();
+    entry_sums<L>(a, l, tm, m, en, s);
+    row_red<L>(s, shs, Sum());
+    if (L == 64) row_sync<L>();
+    const bool labelled = HARD && en.cls[a.K] >= 0;
+    if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
     if (dr) {
-      const float f = a.scale * w;
-      const float ft = soft_on ? f * a.alpha * a.temperature : 0.f, fh = hard_on ? f * (1.0f - a.alpha) : 0.f;
-      auto grad = [&](float zv) {
-        const float d = zv - m;
-        float g = 0.f;
-        if (soft_on) g += ft * (expf(d * invt) / st);
-        if (hard_on) g += fh * (expf(d) / s1);
-        return g;
-      };
-      // the named classes' values, before dz (which may replace z) is written
-      float gk = 0.f, gy = 0.f;
-      bool own_k = false, own_y = false;
-      int at = -1;
-      const int k = threadIdx.x;
-      if (soft_on && k < a.K && qi[k] >= 0) {
-        at = qi[k];
-        own_k = true;
-        float sum = 0.f;
-        for (int j = 0; j < a.K; ++j)
-          if (qi[j] == at) {
-            if (j < k) own_k = false;
-            sum += q[j];
-          }
-        gk = grad(TT<T>::to_f(zr[at])) - ft * (sum / ts) - (hard_on && at == lab ? fh : 0.f);
+      const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float v[VW];
+        unpack<T>(q[e], v);
+#pragma unroll
+        for (int j = 0; j < VW; ++j) v[j] = grad_at<HARD>(g, v[j]);
+        if (e * L + l < nch) store_chunk(dr + (e * L + l) * VW, pack<T>(v));
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (hard_on && threadIdx.x == 0) {
-        own_y = true;
-        for (int j = 0; soft_on && j < a.K; ++j) own_y &= qi[j] != lab;
-        gy = grad(TT<T>::to_f(zr[lab])) - fh;
-      }
-      __syncthreads();
-      for (int c = threadIdx.x; c < a.C; c += 256) dr[c] = TT<T>::from_f(grad(TT<T>::to_f(zr[c])));
-      __syncthreads();
-      if (own_k) dr[at] = TT<T>::from_f(gk);
-      if (own_y) dr[lab] = TT<T>::from_f(gy);
+      if (tail < a.C) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, zt));
+      row_sync<L>();   // the named classes are written after the rest
+      write_entries<T, L, HARD>(a, l, g, en, dr, 0, a.C);
     }
+    row_sync<L>();   // before the next row's entries
+  }
+}
+
+// Rows in parts, a block of 256 threads each: the first launch leaves each
+// part's maximum and sums, and the student's logits of the row's entries, the
+// second joins them and writes the gradient of its part.
+//   ws[row]: (m, sum exp(z'), sum exp(z - m), -) of each part, then the K + 1 logits
+struct Parts {
+  float* ws;
+  int n, chunks;   // parts of a row, chunks of a part
+  __host__ __device__ long row_floats(int K) const { return 4l * n + K + 1; }
+};
+
+constexpr int kPartE = 4;   // chunks of a lane in flight
+
+template <typename T, bool HARD>
+__global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, Parts ps) {
+  constexpr int VW = TT<T>::VW, L = 256;
+  __shared__ Entries en;
+  __shared__ float shm[L / 64][1], shs[L / 64][2];
+  const int l = threadIdx.x, nch = a.C / VW;
+  const int c0 = (int)blockIdx.x * ps.chunks, c1 = std::min(nch, c0 + ps.chunks);
+  const bool last = (int)blockIdx.x == ps.n - 1;
+  const float ct = kLog2e / a.temperature;
+  for (long r = blockIdx.y; r < a.R; r += gridDim.y) {
+    if (a.weight && a.weight[r] == 0.f) continue;
+    const T* zr = (const T*)a.z + r * a.ldz;
+    float* wr = ps.ws + r * ps.row_floats(a.K);
+    if (blockIdx.x == 0) {
+      load_entries<T, L, HARD>(a, r, l, zr, nullptr, en);
+      for (int k = l; k <= a.K; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
+    }
+    const int tail = nch * VW + l;
+    // a running maximum of the lane, and its sums relative to it
+    float m = last && tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
+    float s[2] = {m == -INFINITY ? 0.f : 1.f, HARD && m != -INFINITY ? 1.f : 0.f};
+    if (m != m) s[0] = s[1] = m;
+    for (int b = c0 + l; b < c1; b += L * kPartE) {
+      uint4 q[kPartE];
+      float v[kPartE][VW], top = m;
+#pragma unroll
+      for (int e = 0; e < kPartE; ++e) q[e] = load_chunk(zr + (long)std::min(b + e * L, c1 - 1) * VW);
+#pragma unroll
+      for (int e = 0; e < kPartE; ++e) {
+        unpack<T>(q[e], v[e]);
+        top = max2(top, chunk_max<VW>(v[e]));   // (a chunk past the part is one of the part)
+      }
+      if (top == -INFINITY) continue;
+      if (top != m) {
+        s[0] *= exp2_hw((m - top) * ct);
+        s[1] *= exp2_hw((m - top) * kLog2e);
+        m = top;
+      }
+#pragma unroll
+      for (int e = 0; e < kPartE; ++e)
+        if (b + e * L < c1)
+#pragma unroll
+          for (int j = 0; j < VW; ++j) {
+            s[0] += exp2_hw((v[e][j] - m) * ct);
+            if (HARD) s[1] += exp2_hw((v[e][j] - m) * kLog2e);
+          }
+    }
+    float mx[1] = {m};
+    row_red<L>(mx, shm, Max());
+    const float all = mx[0] == -INFINITY ? 0.f : mx[0];
+    if (m == -INFINITY) m = all;   // sums of zero
+    s[0] *= exp2_hw((m - all) * ct);
+    s[1] *= exp2_hw((m - all) * kLog2e);
+    row_red<L>(s, shs, Sum());
+    if (l == 0) {
+      float* o = wr + 4 * blockIdx.x;
+      o[0] = mx[0];
+      o[1] = s[0];
+      o[2] = s[1];
+    }
+    __syncthreads();   // before the next row's entries and reductions
+  }
+}
+
+template <typename T, bool HARD>
+__global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, Parts ps) {
+  constexpr int VW = TT<T>::VW, L = 256;
+  __shared__ Entries en;
+  __shared__ float shm[L / 64][2], shs[L / 64][SUMS];
+  const int l = threadIdx.x, nch = a.C / VW;
+  const int c0 = (int)blockIdx.x * ps.chunks, c1 = std::min(nch, c0 + ps.chunks);
+  const bool last = (int)blockIdx.x == ps.n - 1;
+  const float ct = kLog2e / a.temperature;
+  for (long r = blockIdx.y; r < a.R; r += gridDim.y) {
+    const T* zr = (const T*)a.z + r * a.ldz;
+    T* dr = a.dz ? (T*)a.dz + r * a.lddz : nullptr;
+    const float w = a.weight ? a.weight[r] : 1.0f;
+    const int tail = last && nch * VW + l < a.C ? nch * VW + l : -1;
+    if (w == 0.f) {
+      if (blockIdx.x == 0 && l == 0) a.row_loss[r] = 0.f;
+      if (dr) {
+        for (int c = c0 + l; c < c1; c += L) store_chunk(dr + (long)c * VW, make_uint4(0, 0, 0, 0));
+        if (tail >= 0) dr[tail] = TT<T>::from_f(0.f);
+      }
+      continue;
+    }
+    const float* wr = ps.ws + r * ps.row_floats(a.K);
+    float mx[2] = {-INFINITY, load_entries<T, L, HARD>(a, r, l, zr, wr + 4 * ps.n, en)};
+    for (int p = l; p < ps.n; p += L) mx[0] = max2(mx[0], wr[4 * p]);
+    row_red<L>(mx, shm, Max());
+    const float m = mx[0] == -INFINITY ? 0.f : mx[0], tm = mx[1] == -INFINITY ? 0.f : mx[1];
+    float s[SUMS] = {};
+    for (int p = l; p < ps.n; p += L) {
+      const float mp = wr[4 * p];
+      if (mp == -INFINITY) continue;
+      s[SUM_T] += wr[4 * p + 1] * exp2_hw((mp - m) * ct);
+      if (HARD) s[SUM_1] += wr[4 * p + 2] * exp2_hw((mp - m) * kLog2e);
+    }
+    entry_sums<L>(a, l, tm, m, en, s);
+    row_red<L>(s, shs, Sum());
+    const bool labelled = HARD && en.cls[a.K] >= 0;
+    if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
+    if (dr) {
+      const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
+      for (int b = c0 + l; b < c1; b += L * kPartE) {
+        uint4 q[kPartE];
+#pragma unroll
+        for (int e = 0; e < kPartE; ++e)
+          if (b + e * L < c1) q[e] = load_chunk(zr + (long)(b + e * L) * VW);
+#pragma unroll
+        for (int e = 0; e < kPartE; ++e)
+          if (b + e * L < c1) {
+            float v[VW];
+            unpack<T>(q[e], v);
+#pragma unroll
+            for (int j = 0; j < VW; ++j) v[j] = grad_at<HARD>(g, v[j]);
+            store_chunk(dr + (long)(b + e * L) * VW, pack<T>(v));
+          }
+      }
+      if (tail >= 0) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, TT<T>::to_f(zr[tail])));
+      __syncthreads();   // the named classes are written after the rest
+      write_entries<T, L, HARD>(a, l, g, en, dr, c0 * VW, last ? a.C : c1 * VW);
+    }
+    __syncthreads();
   }
 }
 
 // loss = scale * sum of the row losses, added in 64 bits in a fixed order.
-__global__ __launch_bounds__(256) void distill_loss_kernel(const float* __restrict__ row_loss, long R, float scale,
-                                                           float* __restrict__ loss) {
-  __shared__ double sh[256];
+__global__ __launch_bounds__(1024) void distill_loss_kernel(const float* __restrict__ row_loss, long R, float scale,
+                                                            float* __restrict__ loss, unsigned* err) {
+  __shared__ double sh[16];
   double v = 0.0;
-  for (long i = threadIdx.x; i < R; i += 256) v += (double)row_loss[i];
-  sh[threadIdx.x] = v;
+#pragma unroll 8
+  for (long i = threadIdx.x; i < R; i += 1024) v += (double)row_loss[i];
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int s = 128; s > 0; s >>= 1) {
-    if ((int)threadIdx.x < s) sh[threadIdx.x] += sh[threadIdx.x + s];
-    __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) v += sh[i];
+    const float f = (float)(v * (double)scale);
+    loss[0] = f;
+    if (err && !isfinite(f)) atomicOr(err, (unsigned)DEVERR_NONFINITE);
   }
-  if (threadIdx.x == 0) loss[0] = (float)(sh[0] * (double)scale);
+}
+
+// ------------------------------------------------------------------ choice of kernel
+// Parts of a row (1: none). Rows beyond a block's registers, and rows that
+// are too few to fill the chip: as many parts as fill it, of at least 512
+// chunks.
+Parts distill_parts(int prec, long R, int C, float* ws) {
+  const int nch = C / prec_vw(prec), cus = plan_cus();
+  int n = 1;
+  if (nch > 16384) n = ceil_div(nch, 8192);
+  if (nch >= 1024 && R < cus) n = std::max(n, std::min(nch / 512, ceil_div(2l * cus, std::max(R, 1l))));
+  n = std::min(n, 4096);
+  const int chunks = ceil_div(std::max(nch, 1), n);
+  return {ws, ceil_div(std::max(nch, 1), chunks), chunks};
+}
+
+template <typename T, bool HARD>
+int distill_go(const DistillArgs& a, const Parts& ps, hipStream_t s) {
+  if (ps.n > 1) {
+    const dim3 grid(ps.n, (unsigned)std::min(a.R, 65535l));
+    hipLaunchKernelGGL((distill_part_stats_kernel<T, HARD>), grid, dim3(256), 0, s, a, ps);
+    hipLaunchKernelGGL((distill_part_grad_kernel<T, HARD>), grid, dim3(256), 0, s, a, ps);
+    return ok();
+  }
+  const int nch = a.C / TT<T>::VW;
+  auto go = [&](auto l, auto e) {
+    constexpr int L = decltype(l)::value, NT = L > 256 ? L : 256, G = NT / L;
+    hipLaunchKernelGGL((distill_row_kernel<T, L, decltype(e)::value, HARD>),
+                       dim3((unsigned)std::min((a.R + G - 1) / G, 1l << 22)), dim3(NT), 0, s, a);
+    return ok();
+  };
+#define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{})
+  if (nch <= 256 && a.R >= 4l * plan_cus()) {
+    if (nch <= 64) GO(64, 1);
+    if (nch <= 128) GO(64, 2);
+    GO(64, 4);
+  }
+  if (nch <= 256) GO(256, 1);
+  if (nch <= 512) GO(256, 2);
+  if (nch <= 1024) GO(256, 4);
+  if (nch <= 2048) GO(256, 8);
+  if (nch <= 4096) GO(512, 8);
+  if (nch <= 8192) GO(512, 16);
+  GO(1024, 16);
+#undef GO
 }
 
 }  // namespace
 
 size_t distill_workspace(int prec, long R, int C, int K) {
-  (void)prec; (void)R; (void)C; (void)K;
-  return 0;
+  const Parts ps = distill_parts(prec, R, C, nullptr);
+  return ps.n > 1 && R > 0 ? (size_t)R * ps.row_floats(K) * 4 : 0;
 }
 
 int distill_launch(int prec, const DistillArgs& a, float* loss, void* ws, hipStream_t s) {
-  (void)ws;
-  return with_prec(prec, [&](auto tag) {
-    using T = decltype(tag);
-    if (a.R > 0) hipLaunchKernelGGL(distill_kernel<T>, dim3(row_grid(a.R)), dim3(256), 0, s, a);
-    if (loss) hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(256), 0, s, a.row_loss, a.R, a.scale, loss);
+  if (a.R > 0) {
+    const Parts ps = distill_parts(prec, a.R, a.C, (float*)ws);
+    const int r = with_prec(prec, [&](auto tag) {
+      using T = decltype(tag);
+      return a.labels && a.alpha != 1.0f ? distill_go<T, true>(a, ps, s) : distill_go<T, false>(a, ps, s);
+    });
+    if (r) return r;
+  }
+  if (loss) {
+    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(1024), 0, s, a.row_loss, a.R, a.scale, loss, a.err);
     return ok();
-  });
+  }
+  return 0;
 }
 
 }  // namespace rn18

@@ -301,6 +301,11 @@ struct DistillArgs {
   long R, ldz, lddz;
   int C, K;
   float temperature, alpha, scale;
+  // of a training step (both may be NULL): the context's sticky error flags,
+  // set for a label outside [0, C) or a class of the list that is neither in
+  // there nor -1, and its loss scale, a factor of dz
+  unsigned* err;
+  const LossScale* ls;
 };
 size_t distill_workspace(int prec, long R, int C, int K);
 int distill_launch(int prec, const DistillArgs& a, float* loss, void* ws, hipStream_t s);

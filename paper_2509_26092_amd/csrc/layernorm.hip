@@ -25,28 +25,6 @@ namespace {
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
 // ------------------------------------------------------------------ rows in registers
-// Sums over the L lanes that hold a row. Lanes of more than one wave meet in
-// `sh`, a buffer of the caller that no lane may still read from: callers
-// alternate between two.
-template <int L, int N>
-__device__ inline void row_sums(float (&v)[N], float (*sh)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = group_sum<(L < 64 ? L : 64)>(v[i]);
-  if (L > 64) {
-    const int w = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) sh[w][i] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = sh[0][i];
-#pragma unroll
-      for (int k = 1; k < L / 64; ++k) v[i] += sh[k][i];
-    }
-  }
-}
-
 template <int VW>
 __device__ inline void load_param(const float* p, int start, float fill, float* v) {
 #pragma unroll

@@ -61,13 +61,70 @@ __device__ inline float group_red(float v, F f) {
   }
   return v;
 }
+struct Sum {
+  __device__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+  __device__ float operator()(float a, float b) const { return __builtin_elementwise_maximum(a, b); }
+};
 template <int L>
 __device__ inline float group_sum(float v) {
-  return group_red<L>(v, [](float a, float b) { return a + b; });
+  return group_red<L>(v, Sum());
 }
 template <int L>
 __device__ inline float group_max(float v) {
-  return group_red<L>(v, [](float a, float b) { return fmaxf(a, b); });
+  return group_red<L>(v, Max());
+}
+
+// The same over the L lanes of a row, N values at a time. Lanes of more than
+// one wave meet in `sh`, a buffer of the caller that no lane may still read
+// from: callers alternate between two.
+template <int L, int N, typename F>
+__device__ inline void row_red(float (&v)[N], float (*sh)[N], F f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = group_red<(L < 64 ? L : 64)>(v[i], f);
+  if (L > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sh[w][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = sh[0][i];
+#pragma unroll
+      for (int k = 1; k < L / 64; ++k) v[i] = f(v[i], sh[k][i]);
+    }
+  }
+}
+template <int L, int N>
+__device__ inline void row_sums(float (&v)[N], float (*sh)[N]) {
+  row_red<L>(v, sh, Sum());
+}
+
+// The largest of two and of three, or a NaN if one of them is (one
+// instruction).
+__device__ inline float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ inline float max3(float a, float b, float c) {
+  return max2(max2(a, b), c);
+}
+template <int VW>
+__device__ inline float chunk_max(const float* v) {
+  float m = max3(v[0], v[1], v[2]);
+#pragma unroll
+  for (int j = 3; j + 1 < VW; j += 2) m = max3(m, v[j], v[j + 1]);
+  return max2(m, v[VW - 1]);
+}
+// Between writes and reads of the row's shared memory.
+template <int L>
+__device__ inline void row_sync() {
+  if (L > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
 }
 
 }  // namespace rn18

@@ -37,17 +37,6 @@ __device__ inline float key_value(uint32_t k) {
   return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// The largest of a, b and c, or a NaN if one of them is (one instruction).
-__device__ inline float max3(float a, float b, float c) {
-  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
-}
-template <int VW>
-__device__ inline float chunk_max(const float* v) {
-  float m = max3(v[0], v[1], v[2]);
-#pragma unroll
-  for (int j = 3; j + 1 < VW; j += 2) m = max3(m, v[j], v[j + 1]);
-  return __builtin_elementwise_maximum(m, v[VW - 1]);
-}
 // The key of a maximum that a bound may rest on: 0 for a NaN's.
 __device__ inline uint32_t max_key(float m) { return m == m ? order_key(m) : 0; }
 
@@ -88,18 +77,6 @@ struct TopShared {
   uint32_t count, chunks, bound;
   int part[16];
 };
-
-// Between writes and reads of the row's shared memory.
-template <int L>
-__device__ inline void row_sync() {
-  if (L > 64) {
-    __syncthreads();
-  } else {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
-}
 
 // Sum over the row's waves of a count that each holds, and the sum over the
 // waves before this one.
@@ -183,12 +160,12 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
       float top = tail < C ? vt : -INFINITY;
       if constexpr (REG) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) top = __builtin_elementwise_maximum(top, tops[e]);
+        for (int e = 0; e < E; ++e) top = max2(top, tops[e]);
       } else {
         float v[VW];
         for (int c = l; c < nch; c += L) {
           unpack<T>(load_chunk(zc + (long)c * VW), v);
-          top = __builtin_elementwise_maximum(top, chunk_max<VW>(v));
+          top = max2(top, chunk_max<VW>(v));
         }
       }
       const bool fours = K * 8 <= L;
