@@ -172,9 +172,9 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
       continue;
     }
     uint4 q[E];
+    const T* zc = chunk_base(zr, nch);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      q[e] = nch ? load_chunk_at(zr, (e * L + l < nch ? e * L + l : 0) * 16u) : make_uint4(0, 0, 0, 0);
+    for (int e = 0; e < E; ++e) q[e] = load_chunk_at(zc, (e * L + l < nch ? e * L + l : 0) * 16u);
     const float zt = tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
     float mx[2] = {zt, load_entries<T, L, HARD>(a, r, l, zr, nullptr, en)};
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
         unpack<T>(q[e], v);
 #pragma unroll
         for (int j = 0; j < VW; ++j) v[j] = grad_at<HARD>(g, v[j]);
-        if (e * L + l < nch) store_chunk(dr + (e * L + l) * VW, pack<T>(v));
+        if (e * L + l < nch) store_chunk_at(dr, (e * L + l) * 16u, pack<T>(v));
         __builtin_amdgcn_sched_barrier(0);
       }
       if (tail < a.C) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, zt));

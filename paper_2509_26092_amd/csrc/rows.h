@@ -26,9 +26,22 @@ template <typename T>
 __device__ inline void store_chunk(T* p, const uint4& q) {
   __builtin_memcpy(p, &q, 16);
 }
+template <typename T>
+__device__ inline void store_chunk_at(T* row, uint32_t bytes, const uint4& q) {
+  __builtin_memcpy((T*)((char*)row + bytes), &q, 16);
+}
 
 // A row of W elements is W / VW whole chunks and up to VW - 1 further
 // elements, its tail, one to a lane.
+
+// Where a lane without a chunk of a row loads from: the row's first chunk, or
+// 16 bytes of zeros where the row has none (a branch around the loads would
+// wait for each of them).
+static __device__ const uint4 kNoChunk = {0, 0, 0, 0};
+template <typename T>
+__device__ inline const T* chunk_base(const T* row, int nch) {
+  return nch > 0 ? row : (const T*)&kNoChunk;
+}
 
 // Hides where a chunk came from, so that values unpacked from it before are
 // not kept in registers until they are needed again.
@@ -90,11 +103,7 @@ __device__ inline void row_red(float (&v)[N], float (*sh)[N], F f) {
       for (int i = 0; i < N; ++i) sh[w][i] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = sh[0][i];
-#pragma unroll
-      for (int k = 1; k < L / 64; ++k) v[i] = f(v[i], sh[k][i]);
-    }
+    for (int i = 0; i < N; ++i) v[i] = group_red<(L > 64 ? L / 64 : 1)>(sh[threadIdx.x & (L / 64 - 1)][i], f);
   }
 }
 template <int L, int N>

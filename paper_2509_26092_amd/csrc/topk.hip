@@ -134,13 +134,11 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
       constexpr int B = E < 8 ? E : 8;   // chunks in flight
 #pragma unroll
       for (int e0 = 0; e0 < E; e0 += B) {
-        uint4 q[B] = {};
-        if (nch > 0) {
+        uint4 q[B];
 #pragma unroll
-          for (int e = 0; e < B; ++e) {
-            const int c = (e0 + e) * L + l;
-            q[e] = load_chunk_at(zc, (c < nch ? c : 0) * 16u);
-          }
+        for (int e = 0; e < B; ++e) {
+          const int c = (e0 + e) * L + l;
+          q[e] = load_chunk_at(chunk_base(zc, nch), (c < nch ? c : 0) * 16u);
         }
 #pragma unroll
         for (int e = 0; e < B; ++e) {
