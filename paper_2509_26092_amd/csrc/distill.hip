@@ -30,11 +30,13 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // 2^x by the hardware's instruction (1 ulp; 0 below 2^-126)
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The teacher's list of a row and, as entry K, the label.
-struct Entries {
-  int32_t cls[kTopMax + 1];   // -1: not valid
+// The teacher's list of a row and, as entry K, the label; the class of the
+// label is apart, and -1 fills the list's classes up to a multiple of 4.
+struct alignas(16) Entries {
+  int32_t cls[kTopMax];       // -1: not valid
   float e[kTopMax + 1];       // t / T, then exp(t / T - their maximum)
   float z[kTopMax + 1];       // the student's logit
+  int32_t label;
 };
 
 // Loads a row's entries; zk: the student's logits of the entries, if they
@@ -62,11 +64,13 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
         i = -1;
       }
     }
-    en.cls[k] = i;
+    if (k < a.K) en.cls[k] = i;
+    else en.label = i;
     en.e[k] = t;
     en.z[k] = i < 0 ? 0.f : zk ? zk[k] : TT<T>::to_f(zr[i]);
     tm = max2(tm, t);
   }
+  if (l < ((4 - (a.K & 3)) & 3)) en.cls[a.K + l] = -1;
   if (a.err && bad) atomicOr(a.err, (unsigned)DEVERR_LABEL);
   return tm;
 }
@@ -84,7 +88,6 @@ __device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m
     s[SUM_Q] += e;
     if (e != 0.f) s[SUM_QD] += e * (t - (en.z[k] - m) * invt);
   }
-  if (l == 0) en.e[a.K] = 0.f;
 }
 
 // What the gradient of a row needs: dz_j = exp(z') gt + exp(z - m) g1, less
@@ -119,7 +122,7 @@ __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* 
   const bool some = s[SUM_T] != 0.f;
   float v = 0.f;
   if (some && s[SUM_Q] != 0.f)
-    v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] - logf(s[SUM_Q]) + logf(s[SUM_T]));
+    v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] + logf(s[SUM_T] / s[SUM_Q]));
   if (HARD && some && labelled) v += (1.0f - a.alpha) * (logf(s[SUM_1]) - (zlab - m));
   return w * v;
 }
@@ -130,18 +133,27 @@ template <typename T, int L, bool HARD>
 __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries& en, T* dr, int c0,
                                      int c1) {
   for (int k = l; k <= a.K; k += L) {
-    const int at = en.cls[k];
+    const int at = k < a.K ? en.cls[k] : en.label;
+    // entries of the same class, itself among them: most lists have none
+    int same = 0;
+    for (int j = 0; j < a.K; j += 4) {
+      const int4 c = *(const int4*)(en.cls + j);
+      same += (c.x == at ? 1 : 0) + (c.y == at ? 1 : 0) + (c.z == at ? 1 : 0) + (c.w == at ? 1 : 0);
+    }
     if (at < c0 || at >= c1) continue;
-    bool first = true;
-    float q = 0.f;
-    for (int j = 0; j < a.K; ++j)
-      if (en.cls[j] == at) {
-        first &= j >= k;
-        q += en.e[j];
-      }
-    if (!first) continue;
+    float q = k < a.K ? en.e[k] : 0.f;
+    if (same > (k < a.K ? 1 : 0)) {
+      bool first = true;
+      q = 0.f;
+      for (int j = 0; j < a.K; ++j)
+        if (en.cls[j] == at) {
+          first &= j >= k;
+          q += en.e[j];
+        }
+      if (!first) continue;
+    }
     float v = grad_at<HARD>(g, en.z[k]) - g.fq * q;
-    if (HARD && at == en.cls[a.K]) v -= g.fh;
+    if (HARD && at == en.label) v -= g.fh;
     dr[at] = TT<T>::from_f(v);
   }
 }
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
     entry_sums<L>(a, l, tm, m, en, s);
     row_red<L>(s, shs, Sum());
     if (L == 64) row_sync<L>();
-    const bool labelled = HARD && en.cls[a.K] >= 0;
+    const bool labelled = HARD && en.label >= 0;
     if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
@@ -341,7 +353,7 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
     }
     entry_sums<L>(a, l, tm, m, en, s);
     row_red<L>(s, shs, Sum());
-    const bool labelled = HARD && en.cls[a.K] >= 0;
+    const bool labelled = HARD && en.label >= 0;
     if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
@@ -373,8 +385,13 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(const float* __restr
                                                             float* __restrict__ loss, unsigned* err) {
   __shared__ double sh[16];
   double v = 0.0;
-#pragma unroll 8
-  for (long i = threadIdx.x; i < R; i += 1024) v += (double)row_loss[i];
+#pragma unroll 4
+  for (long i = threadIdx.x; i < R / 4; i += 1024) {
+    float x[4];
+    __builtin_memcpy(x, row_loss + 4 * i, 16);
+    v += ((double)x[0] + (double)x[1]) + ((double)x[2] + (double)x[3]);
+  }
+  if ((long)threadIdx.x < R % 4) v += (double)row_loss[R / 4 * 4 + threadIdx.x];
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -416,10 +433,11 @@ int distill_go(const DistillArgs& a, const Parts& ps, hipStream_t s) {
     return ok();
   };
 #define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{})
-  if (nch <= 256 && a.R >= 4l * plan_cus()) {
+  if (nch <= 512 && a.R >= 4l * plan_cus()) {
     if (nch <= 64) GO(64, 1);
     if (nch <= 128) GO(64, 2);
-    GO(64, 4);
+    if (nch <= 256) GO(64, 4);
+    GO(64, 8);
   }
   if (nch <= 256) GO(256, 1);
   if (nch <= 512) GO(256, 2);
