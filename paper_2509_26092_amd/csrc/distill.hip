@@ -46,7 +46,7 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
   const float invt = 1.0f / a.temperature;
   float tm = -INFINITY;
   bool bad = false;
-  for (int k = l; k <= a.K; k += L) {
+  for (int k = l; k < a.K + HARD; k += L) {   // (the label last)
     float t = -INFINITY;
     int i = -1;
     if (k < a.K) {
@@ -57,7 +57,7 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
         i = -1;
         t = -INFINITY;
       }
-    } else if (HARD) {
+    } else {
       i = a.labels[r];
       if (i < 0 || i >= a.C) {
         bad = true;
@@ -132,7 +132,7 @@ __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* 
 template <typename T, int L, bool HARD>
 __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries& en, T* dr, int c0,
                                      int c1) {
-  for (int k = l; k <= a.K; k += L) {
+  for (int k = l; k < a.K + HARD; k += L) {
     const int at = k < a.K ? en.cls[k] : en.label;
     // entries of the same class, itself among them: most lists have none
     int same = 0;
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
     row_red<L>(s, shs, Sum());
     if (L == 64) row_sync<L>();
     const bool labelled = HARD && en.label >= 0;
-    if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
+    if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, HARD ? en.z[a.K] : 0.f, labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
 #pragma unroll
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, 
     float* wr = ps.ws + r * ps.row_floats(a.K);
     if (blockIdx.x == 0) {
       load_entries<T, L, HARD>(a, r, l, zr, nullptr, en);
-      for (int k = l; k <= a.K; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
+      for (int k = l; k < a.K + HARD; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
     }
     const int tail = nch * VW + l;
     // a running maximum of the lane, and its sums relative to it
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
     entry_sums<L>(a, l, tm, m, en, s);
     row_red<L>(s, shs, Sum());
     const bool labelled = HARD && en.label >= 0;
-    if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, en.z[a.K], labelled);
+    if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, HARD ? en.z[a.K] : 0.f, labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
       for (int b = c0 + l; b < c1; b += L * kPartE) {
@@ -404,14 +404,16 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(const float* __restr
 }
 
 // ------------------------------------------------------------------ choice of kernel
-// Parts of a row (1: none). Rows beyond a block's registers, and rows that
-// are too few to fill the chip: as many parts as fill it, of at least 512
-// chunks.
+// Parts of a row (1: none): for rows beyond a block's registers, and for up
+// to a row for every fourth compute unit, of more than 4096 chunks, which
+// alone take longer than the launch that joins parts (one row of 131072 bf16
+// logits: 12.9 us in parts, 19.4 whole, 64 of them 18.2 and 25.9; of 32768:
+// 12.5 and 10.7; 128 rows of 65536: 20.6 and 19.9).
 Parts distill_parts(int prec, long R, int C, float* ws) {
   const int nch = C / prec_vw(prec), cus = plan_cus();
   int n = 1;
   if (nch > 16384) n = ceil_div(nch, 8192);
-  if (nch >= 1024 && R < cus) n = std::max(n, std::min(nch / 512, ceil_div(2l * cus, std::max(R, 1l))));
+  if (nch > 4096 && R * 4 <= cus) n = std::max(n, std::min(nch / 512, ceil_div(2l * cus, std::max(R, 1l))));
   n = std::min(n, 4096);
   const int chunks = ceil_div(std::max(nch, 1), n);
   return {ws, ceil_div(std::max(nch, 1), chunks), chunks};
