@@ -36,8 +36,9 @@ __device__ inline void store_chunk_at(T* row, uint32_t bytes, const uint4& q) {
 
 // Where a lane without a chunk of a row loads from: the row's first chunk, or
 // 16 bytes of zeros where the row has none (a branch around the loads would
-// wait for each of them).
-static __device__ const uint4 kNoChunk = {0, 0, 0, 0};
+// wait for each of them). Not const: global memory like the rows, so that the
+// loads are global ones.
+static __device__ uint4 kNoChunk = {0, 0, 0, 0};
 template <typename T>
 __device__ inline const T* chunk_base(const T* row, int nch) {
   return nch > 0 ? row : (const T*)&kNoChunk;
