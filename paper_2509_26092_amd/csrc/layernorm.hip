@@ -150,10 +150,70 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_fwd_kernel(const T* x, c
 // registers over all its rows, joins them over the block's row groups, and
 // writes one partial row per block: part[block][2][Dp] (Dp = D rounded up to
 // 4).
+// Small calls take one launch instead: dgamma and dbeta need no row sums, so
+// blocks of their own (from row_blocks on) add up 32 columns each over all
+// rows, beside the blocks that write dx.
 struct LnParamOut {
-  float* part;     // NULL: no parameter gradient is wanted
+  float* part;     // NULL: no parameter gradient is wanted, or blocks of their own write them
   int Dp;
+  int row_blocks;
+  float *dgamma, *dbeta;
 };
+
+// Sums over the rows of 32 columns from c0: 8 lanes of 4 columns by 32 groups
+// of rows (the block's first 256 threads), the groups' sums by fours and the
+// fours in order.
+template <typename T>
+__device__ inline void ln_columns(const T* dy, const T* x, const float* mean, const float* rstd, float* dgamma,
+                                  float* dbeta, long R, int D, long lddy, long ldx, int c0) {
+  __shared__ float sh[2][32][33], sh2[2][8][33];
+  const int t = threadIdx.x, cl = (t & 7) * 4, rg = t >> 3, c = c0 + cl;
+  float g[4] = {}, b[4] = {};
+  if (t < 256 && c < D) {
+#pragma unroll 4
+    for (long r = rg; r < R; r += 32) {
+      const float m = mean[r], rs = rstd[r];
+      T qd[4] = {}, qx[4] = {};
+      if (c + 4 <= D) {
+        __builtin_memcpy(qd, dy + r * lddy + c, 4 * sizeof(T));
+        __builtin_memcpy(qx, x + r * ldx + c, 4 * sizeof(T));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (j < D - c) {
+            qd[j] = dy[r * lddy + c + j];
+            qx[j] = x[r * ldx + c + j];
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float d = TT<T>::to_f(qd[j]);
+        b[j] += d;
+        g[j] += d * ((TT<T>::to_f(qx[j]) - m) * rs);
+      }
+    }
+  }
+  if (t < 256)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sh[0][rg][cl + j] = g[j];
+      sh[1][rg][cl + j] = b[j];
+    }
+  __syncthreads();
+  const int k = t & 31, q = t >> 5;
+  if (t < 256)
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      sh2[w][q][k] = (sh[w][4 * q][k] + sh[w][4 * q + 1][k]) + (sh[w][4 * q + 2][k] + sh[w][4 * q + 3][k]);
+  __syncthreads();
+  float* o = q == 0 ? dgamma : dbeta;
+  if (q < 2 && c0 + k < D && o) {
+    float v = sh2[q][0][k];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += sh2[q][i][k];
+    o[c0 + k] = v;
+  }
+}
 
 // WIDE: for the widest rows, whose column sums would not fit in registers
 // beside two rows: the sums live in LDS (each lane adds to its own columns)
@@ -167,6 +227,10 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, 
                                                                    long lddx) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L, NW = NT / 64;
   constexpr int NV = 2 * (E * VW + 1);
+  if (!WIDE && (int)blockIdx.x >= po.row_blocks) {
+    ln_columns(dy, x, mean, rstd, po.dgamma, po.dbeta, R, D, lddy, ldx, ((int)blockIdx.x - po.row_blocks) * 32);
+    return;
+  }
   // joining of the row groups: a wave's own in registers, the waves' here
   __shared__ float shp[L > 64 ? 1 : NW][L > 64 ? 1 : L * NV];
   __shared__ float sh[2][L > 64 ? L / 64 : 1][2];
@@ -186,7 +250,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, 
 #pragma unroll
   for (int i = 0; i <= E * VW; ++i) ag[i] = ab[i] = 0.f;
   const float fd = (float)D;
-  const long step = (long)gridDim.x * G;
+  const long step = (long)po.row_blocks * G;
   long r = (long)blockIdx.x * G + g;
   uint4 qd[E], qx[E], nd[E], nx[E];
   T td, tx, ntd, ntx;
@@ -583,7 +647,9 @@ LnPath ln_tile(int prec, int D, int max_e, int* L, int* E) {
     if (nch <= l * max_e) {
       *L = l;
       *E = ceil_div(nch, l);
-      return LN_TILE;
+      // (32 columns a lane beside gamma and beta do not fit in a lane's 128
+      // registers: 2000x32768 bf16 forward 91 us, as a long row 85)
+      return l == 1024 && *E * vw > 24 ? LN_LONG : LN_TILE;
     }
   return LN_LONG;
 }
@@ -633,7 +699,8 @@ int fwd_tile(int L, int E, long R, hipStream_t s, A... a) {
     case 512 * 8 + 3: return fwd_go<T, 512, 3, 1>(R, s, a...);
     case 512 * 8 + 4: return fwd_go<T, 512, 4, 1>(R, s, a...);
     case 1024 * 8 + 3: return fwd_go<T, 1024, 3, 1>(R, s, a...);
-    case 1024 * 8 + 4: return fwd_go<T, 1024, 4, 1>(R, s, a...);
+    case 1024 * 8 + 4:
+      if constexpr (TT<T>::VW == 4) return fwd_go<T, 1024, 4, 1>(R, s, a...);
     default: return -1;
   }
 }
@@ -714,6 +781,15 @@ int layernorm_fwd_launch(int prec, const void* x, const float* gamma, const floa
   });
 }
 
+// Calls whose parameter gradients blocks of their own add up, in place of a
+// second launch that joins partial sums: dy and x are read twice, from cache,
+// and a column's sum is a chain of R / 32 additions. (A call on 64x512 fp32:
+// 6.1 us, with the second launch 9.7; 512x8192 bf16 13.0 and 20.4; but
+// 2048x1024 bf16 13.3 and 9.4.)
+static bool ln_bwd_small(int prec, long R, int D) {
+  return R <= 1024 && R * D * prec_bytes(prec) <= (8l << 20);
+}
+
 size_t layernorm_bwd_workspace(int prec, long R, int D) {
   if (R <= 0) return 0;
   int L = 0, E = 0;
@@ -728,14 +804,16 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
   const LnPath path = ln_tile(prec, D, bwd_max_e(prec), &L, &E);
   const bool params = dgamma || dbeta;
   const int grid = R > 0 ? bwd_grid(path, L, R, D) : 0;
-  const LnParamOut po{params ? (float*)ws : nullptr, (D + 3) & ~3};
+  // (dx in place of dy or x would be written while the column sums read them)
+  const bool small = params && R > 0 && path == LN_TILE && L < 1024 && dx != dy && dx != x && ln_bwd_small(prec, R, D);
+  const LnParamOut po{params && !small ? (float*)ws : nullptr, (D + 3) & ~3, grid, dgamma, dbeta};
   if (R > 0) {
     const int r = with_prec(prec, [&](auto tag) {
       using T = decltype(tag);
       const T *dyt = (const T*)dy, *xt = (const T*)x;
       T* dxt = (T*)dx;
       if (path == LN_TILE)
-        return bwd_tile<T>(L, E, grid, s, dyt, xt, gamma, mean, rstd, dxt, po, R, D, lddy, ldx, lddx);
+        return bwd_tile<T>(L, E, small ? grid + ceil_div(D, 32) : grid, s, dyt, xt, gamma, mean, rstd, dxt, po, R, D, lddy, ldx, lddx);
       if (path == LN_SHORT) {
         hipLaunchKernelGGL(ln_bwd_short_kernel<T>, dim3(grid), dim3(256), 0, s, dyt, xt, gamma, mean, rstd, dxt, po, R,
                            D, lddy, ldx, lddx);
@@ -750,7 +828,7 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
     });
     if (r) return r;
   }
-  if (params) {
+  if (params && !small) {
     hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(po.Dp, 32), 2), dim3(1024), 0, s, (const float*)ws, grid, D,
                        po.Dp, dgamma, dbeta);
     return ok();
