@@ -27,8 +27,9 @@ inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
 // Order-preserving unsigned key of a float: larger value, larger key; the
 // two zeros share a key and every NaN has the largest one. 0 is no value's.
+constexpr uint32_t kNanKey = 0xfffffffeu;
 __device__ inline uint32_t order_key(float v) {
-  if (v != v) return 0xfffffffeu;
+  if (v != v) return kNanKey;
   const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.0f);   // -0 + 0 = +0
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
@@ -37,6 +38,13 @@ __device__ inline float key_value(uint32_t k) {
   return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
+// A value such that the numbers above it are those with keys above k, for k
+// from -inf's key on: -0's own pattern is no number's key, and above +inf
+// there are only NaNs.
+__device__ inline float above_value(uint32_t k) {
+  if (k == 0x7fffffffu) --k;
+  return k >= 0xff800000u ? INFINITY : key_value(k);
+}
 // The key of a maximum that a bound may rest on: 0 for a NaN's.
 __device__ inline uint32_t max_key(float m) { return m == m ? order_key(m) : 0; }
 
@@ -235,36 +243,49 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
     row_sync<L>();
     int n = hits <= M ? (int)sh.count : M + 1;
     if (n > M) {
-      // (one logit at a time: few rows come here, and the registers of the
-      // common path set how many rows are in flight)
-      auto above = [&](uint32_t k) {   // count of logits above a key
-        int s = 0, before;
-#pragma unroll 4
-        for (int c = l; c - l < C; c += L)
-          s += __popcll(__ballot(c < C && order_key(TT<T>::to_f(zr[c < C ? c : 0])) > k));
-        return row_count<L>(s, &before, sh);
+      // the list of the logits above a key, and their count
+      auto above = [&](uint32_t k) {
+        row_sync<L>();
+        if (l == 0) sh.count = 0;
+        row_sync<L>();
+        const float v0 = above_value(k);   // above k: not at or below v0
+        if (k < kNanKey) {
+#pragma unroll 1
+          for (int c = l; c < nch; c += L) {
+            float v[VW];
+            unpack<T>(load_chunk(zc + (long)c * VW), v);
+            if (chunk_max<VW>(v) <= v0) continue;
+            uint32_t hit = 0;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) hit |= !(v[j] <= v0) ? 1u << j : 0u;
+            uint32_t at = atomicAdd(&sh.count, (uint32_t)__popc(hit));
+#pragma unroll 1
+            for (; hit; hit &= hit - 1, ++at) {
+              const int i = head + c * VW + __ffs(hit) - 1;
+              if (at < M) sh.list[at] = (uint64_t)order_key(TT<T>::to_f(zr[i])) << 32 | (uint32_t)~i;
+            }
+          }
+          if (tail < C && !(vt <= v0)) take(vt, tail);
+        }
+        row_sync<L>();
+        return (int)sh.count;
       };
       // above(lo) > M, above(hi) < K; the bound's own key is the likely answer
       uint32_t lo = order_key(bound) - 1, hi = 0xffffffffu, at = lo + 1;
       int have = 0;
 #pragma unroll 1
-      while (hi - lo > 1) {
+      while (true) {
         have = above(at);
         if (have > M) lo = at;
         else if (have < K) hi = at;
         else break;
+        if (hi - lo <= 1) break;
         at = lo + (hi - lo) / 2;
       }
-      if (hi - lo <= 1) {   // all above hi, and the first classes at hi
+      if (have > M) {   // all above hi, and the first classes at hi
         at = hi;
         have = above(at);
       }
-      row_sync<L>();
-      if (l == 0) sh.count = 0;
-      row_sync<L>();
-#pragma unroll 1
-      for (int c = l; c < C; c += L)
-        if (const float v = TT<T>::to_f(zr[c]); order_key(v) > at) take(v, c);
       n = have;
 #pragma unroll 1
       for (int c0 = 0; c0 < C && n < K; c0 += L) {
