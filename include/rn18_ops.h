@@ -80,8 +80,8 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* hip_stream);
 
 /* ---- Row operators -------------------------------------------------------
  * Layer norm, a teacher's top logits and the distillation loss work on R rows
- * of a matrix whose rows are `ld` elements apart (ld >= the width; any ld and
- * any width >= 1). Their tensors of the storage type need only the alignment
+ * of a matrix whose rows are `ld` elements apart (ld >= the width; any ld, any
+ * width from 1 to 2^30). Their tensors of the storage type need only the alignment
  * of one element, their fp32 and int32 arrays that of 4 bytes; rows may be of
  * any number whose tensors span at most 2^46 elements, R = 0 included. `prec`
  * may be RN18_FP16 too. Sums, statistics and the loss are fp32 or wider, and

@@ -1720,6 +1720,7 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* stream) {
 // ---------------------------------------------------------------------------
 namespace {
 constexpr int64_t kMaxRowElems = (int64_t)1 << 46;   // rows x stride of one tensor
+constexpr int kMaxWidth = 1 << 30;                   // of a row: its positions, with a block's lanes added, are ints
 
 // Rows x width of a tensor with row stride ld, elements of the storage type.
 int rows_check(int prec, const char* name, const void* p, int64_t R, int width, int64_t ld) {
@@ -1744,6 +1745,7 @@ int row_sizes_check(int prec, int64_t R, int width) {
   if (prec != RN18_FP32 && prec != RN18_BF16 && prec != RN18_FP16) return fail(RN18_EINVAL, "bad precision");
   if (R < 0 || R > kMaxRowElems) return fail(RN18_EINVAL, "bad number of rows");
   if (width < 1) return fail(RN18_EINVAL, "non-positive size");
+  if (width > kMaxWidth) return fail(RN18_EINVAL, "rows of more than 2^30 elements");
   return RN18_OK;
 }
 int ws_check(const void* ws, size_t bytes, size_t need) {

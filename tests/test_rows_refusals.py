@@ -88,3 +88,16 @@ def test_workspaces_too_small_or_missing_are_refused(f, need, kw, R, W):
     assert f(R=R, ws=A, ws_bytes=n - 1, **kw(R, W)) == B.RN18_ENOMEM
     assert f(R=R, ws=None, ws_bytes=n, **kw(R, W)) == B.RN18_EINVAL
     assert f(R=R, ws=P((1 << 20) + 4), ws_bytes=n, **kw(R, W)) == B.RN18_EINVAL
+
+
+@pytest.mark.parametrize("W", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_rows_of_more_than_2_30_elements_are_refused(W):
+    """A lane's position past the last chunk would pass 2^31 in the kernels."""
+    big = (1 << 62)
+    assert fwd(R=1, D=W, ldx=W, ldy=W) == B.RN18_EINVAL
+    assert bwd(R=1, D=W, lddy=W, ldx=W, lddx=W, ws_bytes=big) == B.RN18_EINVAL
+    assert topk(R=1, C=W, ldz=W, ws_bytes=big) == B.RN18_EINVAL
+    assert distill(R=1, C=W, ldz=W, lddz=W, ws_bytes=big) == B.RN18_EINVAL
+    assert B.rn18op_layernorm_bwd_workspace(B.RN18_BF16, 1, W) == 0
+    assert B.rn18op_topk_logits_workspace(B.RN18_BF16, 1, W, 4) == 0
+    assert B.rn18op_distill_loss_workspace(B.RN18_BF16, 1, W, 4) == 0
