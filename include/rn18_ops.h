@@ -123,7 +123,7 @@ int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64
 /* Distillation from a teacher's top logits, with the labels' cross-entropy,
  * and the gradient of the student's logits z [R][C]:
  *   P = softmax(z / T), p = softmax(z), q = softmax of t_vals / T over the
- *   row's valid entries (0 <= t_idx < C and t_vals > -inf)
+ *   row's valid entries (0 <= t_idx < C and t_vals not -inf)
  *   row_loss = w * (alpha T^2 sum_k q_k (log q_k - log P[t_idx_k])
  *                   + (1 - alpha) (-log p[label]))
  *   loss = scale * sum of row_loss
@@ -132,7 +132,9 @@ int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64
  * t_vals fp32, t_idx int32 [R][K], 0 <= K <= 256 (K = 0: both may be NULL), in
  * any order; an entry that is not valid is left out (a short list is filled
  * with t_idx = -1), and entries of one class add up. Terms with q_k = 0 are 0.
- * A row without a valid entry has no soft term; one whose label is outside
+ * alpha = 0 leaves out the soft term and alpha = 1 the hard one, whatever
+ * their inputs hold; otherwise a teacher's NaN or +inf makes its row NaN. A
+ * listed class that the student masks has an infinite loss. A row without a valid entry has no soft term; one whose label is outside
  * [0, C) (-1, say; labels NULL: every row) has no hard term; a row whose
  * logits are all -inf (every class masked) has neither. Masked classes hold
  * -inf and get a zero gradient. w: row_weight fp32 [R] (NULL: 1); a row of

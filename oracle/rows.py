@@ -62,7 +62,7 @@ def distill(z, t_vals, t_idx, labels, weight, temperature, alpha, scale):
             continue
         entries = [(int(i), float(t)) for t, i in zip(t_vals[r], t_idx[r]) if 0 <= i < C and t != -np.inf]
         loss, g = 0.0, np.zeros(C)
-        if entries:
+        if entries and alpha != 0.0:
             lq = _log_softmax(np.array([t for _, t in entries]) / temperature)
             lp = _log_softmax(z[r] / temperature)
             g += alpha * temperature * np.exp(lp)

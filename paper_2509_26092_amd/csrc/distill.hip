@@ -60,7 +60,7 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
     } else {
       i = a.labels[r];
       if (i < 0 || i >= a.C) {
-        bad = true;
+        bad |= i != -1;
         i = -1;
       }
     }
@@ -98,7 +98,7 @@ struct RowGrad {
 template <bool HARD>
 __device__ inline RowGrad row_grad(const DistillArgs& a, float w, float m, const float* s, bool labelled) {
   const bool some = s[SUM_T] != 0.f;   // false: every class of the row is masked
-  const bool soft = some && s[SUM_Q] != 0.f, hard = HARD && some && labelled;
+  const bool soft = some && a.alpha != 0.f && s[SUM_Q] != 0.f, hard = HARD && some && labelled;
   const float f = a.scale * w * (a.ls ? a.ls->scale : 1.0f);
   const float ft = f * a.alpha * a.temperature, fh = f * (1.0f - a.alpha);
   RowGrad g;
@@ -121,7 +121,7 @@ template <bool HARD>
 __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* s, float m, float zlab, bool labelled) {
   const bool some = s[SUM_T] != 0.f;
   float v = 0.f;
-  if (some && s[SUM_Q] != 0.f)
+  if (some && a.alpha != 0.f && s[SUM_Q] != 0.f)
     v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] + logf(s[SUM_T] / s[SUM_Q]));
   if (HARD && some && labelled) v += (1.0f - a.alpha) * (logf(s[SUM_1]) - (zlab - m));
   return w * v;

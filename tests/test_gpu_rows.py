@@ -443,6 +443,24 @@ def test_distill_extreme_logits(C):
     assert np.isnan(row[4:6]).all() and np.isnan(dz[4:6]).all() and np.isnan(loss)
 
 
+@pytest.mark.parametrize("C", [10, 1000, 33000, 200000])
+def test_distill_without_the_teachers_term(C):
+    """alpha = 0: the teacher's list, NaN and masked classes in it too, has
+    no part in the loss or the gradient."""
+    R, K = 6, 4
+    z, t_vals, t_idx, labels, _ = distill_inputs("fp32", R, C, K, False, seed=2)
+    t_vals[1], t_vals[2] = np.nan, np.inf
+    for c in t_idx[3]:
+        if c != labels[3]:
+            z[3, c] = -np.inf
+    zd, _ = mat(z, "fp32")
+    dzd, _ = out(R, C, "fp32")
+    row, loss = run_distill(zd, "fp32", t_vals, t_idx, labels, None, K, 2.0, 0.0, 1.0, R, C, C, dzd, C)
+    row_o, loss_o, dz_o = rows.distill(z, t_vals, t_idx, labels, None, 2.0, 0.0, 1.0)
+    assert np.abs(row - row_o).max() <= loss_bound(z, np.zeros(1), None, 2.0, 0.0)
+    assert_close(f64(dzd), dz_o, TOL, "dz")
+
+
 def test_distill_gradient_against_differences_of_the_operator():
     """The loss itself, moved by +-h along random directions in fp32: it is
     about 1 with an error of 1e-6, so at h = 1e-2 the quotient is good to
