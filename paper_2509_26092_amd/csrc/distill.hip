@@ -53,7 +53,7 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
       i = a.t_idx[r * a.K + k];
       t = a.t_vals[r * a.K + k] * invt;
       bad |= i < -1 || i >= a.C;
-      if (i < 0 || i >= a.C || t == -INFINITY) {
+      if (i < 0 || i >= a.C || t == -INFINITY || a.alpha == 0.f) {
         i = -1;
         t = -INFINITY;
       }
@@ -98,7 +98,7 @@ struct RowGrad {
 template <bool HARD>
 __device__ inline RowGrad row_grad(const DistillArgs& a, float w, float m, const float* s, bool labelled) {
   const bool some = s[SUM_T] != 0.f;   // false: every class of the row is masked
-  const bool soft = some && a.alpha != 0.f && s[SUM_Q] != 0.f, hard = HARD && some && labelled;
+  const bool soft = some && s[SUM_Q] != 0.f, hard = HARD && some && labelled;
   const float f = a.scale * w * (a.ls ? a.ls->scale : 1.0f);
   const float ft = f * a.alpha * a.temperature, fh = f * (1.0f - a.alpha);
   RowGrad g;
@@ -121,7 +121,7 @@ template <bool HARD>
 __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* s, float m, float zlab, bool labelled) {
   const bool some = s[SUM_T] != 0.f;
   float v = 0.f;
-  if (some && a.alpha != 0.f && s[SUM_Q] != 0.f)
+  if (some && s[SUM_Q] != 0.f)
     v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] + logf(s[SUM_T] / s[SUM_Q]));
   if (HARD && some && labelled) v += (1.0f - a.alpha) * (logf(s[SUM_1]) - (zlab - m));
   return w * v;
@@ -152,7 +152,8 @@ __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad&
         }
       if (!first) continue;
     }
-    float v = grad_at<HARD>(g, en.z[k]) - g.fq * q;
+    float v = grad_at<HARD>(g, en.z[k]);
+    if (g.fq != 0.f) v -= g.fq * q;   // (a row without a soft term: q may be anything)
     if (HARD && at == en.label) v -= g.fh;
     dr[at] = TT<T>::from_f(v);
   }

@@ -461,6 +461,23 @@ def test_distill_without_the_teachers_term(C):
     assert_close(f64(dzd), dz_o, TOL, "dz")
 
 
+@pytest.mark.parametrize("C", [10, 1000, 33000, 200000])
+def test_distill_masked_rows_whatever_the_teacher_holds(C):
+    """Every class of a row masked: no loss and no gradient, also where the
+    teacher's values are NaN or infinite."""
+    R, K = 3, 4
+    z, t_vals, t_idx, labels, _ = distill_inputs("fp32", R, C, K, False, seed=3)
+    z[0], z[1] = -np.inf, -np.inf
+    t_vals[0], t_vals[1, 2] = np.nan, np.inf
+    zd, _ = mat(z, "fp32")
+    dzd, _ = out(R, C, "fp32")
+    row, loss = run_distill(zd, "fp32", t_vals, t_idx, labels, None, K, 2.0, 0.5, 1.0, R, C, C, dzd, C)
+    row_o, loss_o, dz_o = rows.distill(z, t_vals, t_idx, labels, None, 2.0, 0.5, 1.0)
+    assert row[0] == row[1] == 0.0 and np.abs(row - row_o).max() <= loss_bound(z, t_vals, None, 2.0, 0.5)
+    assert not f64(dzd)[:2].any()
+    assert_close(f64(dzd), dz_o, TOL, "dz")
+
+
 def test_distill_gradient_against_differences_of_the_operator():
     """The loss itself, moved by +-h along random directions in fp32: it is
     about 1 with an error of 1e-6, so at h = 1e-2 the quotient is good to
