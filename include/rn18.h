@@ -32,7 +32,7 @@
  *    step takes up to 21,232 images, more than 288 GB of memory hold; see
  *    rn18_workspace_bytes), or a non-finite factor. rn18_last_error()
  *    returns a thread-local description of the last non-OK return.
- *  - Errors found on the device (a label outside [0, C), a non-finite image
+ *  - Errors found on the device (a bad label, a non-finite image
  *    value or a non-finite loss) set a sticky flag of the context; the call
  *    still runs to completion, and rn18_sync_status reports and clears the
  *    flag.
@@ -129,6 +129,24 @@ int rn18_set_workspace(rn18_ctx* ctx, void* dev, size_t bytes);
 int rn18_train_step(rn18_ctx* ctx, float* state, const float* images, const int32_t* labels, int N, int H, int W,
                     float lr, float* loss);
 
+/* The same step with a teacher: the loss of every sample is the distillation
+ * loss of rn18_ops.h's rn18op_distill_loss,
+ *   alpha T^2 KL(teacher || student at temperature T) + (1 - alpha) CE(label),
+ * averaged over the batch, the teacher given by the K largest of its logits
+ * (what rn18op_topk_logits keeps of rn18_eval_logits).
+ *   t_vals  [N][K] fp32, t_idx [N][K] int32, 1 <= K <= 256; a class of -1
+ *           fills a short list, other classes outside [0, C) are left out and
+ *           set RN18_ELABEL
+ *   labels  [N] int32, -1 for a sample without one (no label term; other
+ *           labels outside [0, C) set RN18_ELABEL too); may be NULL for
+ *           alpha = 1
+ *   temperature > 0, alpha in [0, 1]
+ * Dropout, loss scaling, errors and the update are those of
+ * rn18_train_step. */
+int rn18_train_step_distill(rn18_ctx* ctx, float* state, const float* images, const int32_t* labels,
+                            const float* t_vals, const int32_t* t_idx, int K, float temperature, float alpha, int N,
+                            int H, int W, float lr, float* loss);
+
 /* Forward pass in inference mode (BN with the running statistics in
  * `state`); writes logits [N][C] fp32. */
 int rn18_eval_logits(rn18_ctx* ctx, const float* state, const float* images, int N, int H, int W, float* logits);
@@ -168,7 +186,7 @@ int rn18_set_momentum(rn18_ctx* ctx, const float* src);
  *   t div 2^32), q = (nF + j) div 4, F the feature width;
  * kept features are multiplied by (float)(1 / (1 - p)) and the backward pass
  * applies the same mask. t starts at `step` and advances by one with every
- * successful rn18_train_step (whether or not dropout is on); evaluation never
+ * successful training step (whether or not dropout is on); evaluation never
  * drops. RN18_EINVAL for a NULL ctx or p outside [0, 1). */
 int rn18_set_dropout(rn18_ctx* ctx, float p, uint64_t seed, uint64_t step);
 

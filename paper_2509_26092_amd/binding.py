@@ -28,7 +28,7 @@ EXPORTED = [
     "rn18op_conv2d_fwd", "rn18op_conv2d_dgrad", "rn18op_conv2d_wgrad_workspace", "rn18op_conv2d_wgrad",
     "rn18op_maxpool_fwd", "rn18op_maxpool_bwd", "rn18_debug_set", "rn18_debug_copy",
     "rn18_debug_capture", "rn18op_round_bf16", "rn18op_conv2d_wgrad_noalloc_limit", "rn18op_conv2d_wgrad_noalloc",
-    "rn18op_layernorm_fwd", "rn18op_layernorm_bwd_workspace", "rn18op_layernorm_bwd",
+    "rn18_train_step_distill", "rn18op_layernorm_fwd", "rn18op_layernorm_bwd_workspace", "rn18op_layernorm_bwd",
     "rn18op_topk_logits_workspace", "rn18op_topk_logits", "rn18op_distill_loss_workspace", "rn18op_distill_loss",
 ]
 
@@ -97,6 +97,7 @@ def lib():
         "rn18op_maxpool_fwd": (_I, [_I, _P, _P, _P, _I, _I, _I, _I, _P]),
         "rn18op_maxpool_bwd": (_I, [_I, _P, _P, _P, _I, _I, _I, _I, _P]),
         "rn18op_round_bf16": (_I, [_P, _P, _Z, _P]),
+        "rn18_train_step_distill": (_I, [_P, _P, _P, _P, _P, _P, _I, _F, _F, _I, _I, _I, _F, _P]),
         "rn18op_layernorm_fwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _F, _P]),
         "rn18op_layernorm_bwd_workspace": (_Z, [_I, _L, _I]),
         "rn18op_layernorm_bwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _L, _P, _Z, _P]),
@@ -170,6 +171,11 @@ def rn18_set_workspace(ctx, ws):
 
 def rn18_train_step(ctx, state, images, labels, N, H, W, lr, loss=None):
     return _check(lib().rn18_train_step(ctx, _ptr(state), _ptr(images), _ptr(labels), N, H, W, lr, _ptr(loss)))
+
+
+def rn18_train_step_distill(ctx, state, images, labels, t_vals, t_idx, K, temperature, alpha, N, H, W, lr, loss=None):
+    return _check(lib().rn18_train_step_distill(ctx, _ptr(state), _ptr(images), _ptr(labels), _ptr(t_vals),
+                                                _ptr(t_idx), K, temperature, alpha, N, H, W, lr, _ptr(loss)))
 
 
 def rn18_eval_logits(ctx, state, images, N, H, W, logits):
@@ -374,6 +380,13 @@ class Worker:
         N, _, H, W = images.shape
         self._ensure(N, H, W)
         return rn18_train_step(self.ctx, state, images, labels, N, H, W, lr, loss)
+
+    def train_step_distill(self, state, images, labels, t_vals, t_idx, temperature, alpha, lr, loss=None):
+        """A step against a teacher's top logits t_vals, t_idx [N][K]."""
+        N, _, H, W = images.shape
+        self._ensure(N, H, W)
+        return rn18_train_step_distill(self.ctx, state, images, labels, t_vals, t_idx, t_vals.shape[1], temperature,
+                                       alpha, N, H, W, lr, loss)
 
     def eval_logits(self, state, images, logits):
         N, _, H, W = images.shape

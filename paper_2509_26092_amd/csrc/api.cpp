@@ -181,7 +181,7 @@ struct Plan {
   size_t x0, zstem, pool, parg;
   int Hs, Ws, Hp, Wp;           // stem output and pool output sizes
   int Hf, Wf;                   // final feature map
-  size_t f, logits, dlogits, df, rowloss, lossbuf;
+  size_t f, logits, dlogits, df, rowloss, lossbuf, distill;
   // gy[p], gy2[p]: dY of the second and first conv of the blocks of index
   // parity p (gy[1] also takes the stem's dY); gyd: dY of a projection
   size_t gA, gB, gz, gy[2], gy2[2], gyd;
@@ -449,6 +449,9 @@ int build_plan(const Ctx& c, int N, int H, int W, Plan* pl, std::string* why) {
   pl->df = alloc((size_t)N * a.feat * 4);
   pl->rowloss = alloc((size_t)N * 4);
   pl->lossbuf = alloc(4);
+  // (of a step with a teacher; only few rows of tens of thousands of classes need any)
+  const size_t dws = distill_workspace(RN18_FP32, N, C, kTopMax);
+  pl->distill = dws ? alloc(dws) : 0;
   pl->gA = alloc(max_blockio);
   pl->gB = alloc(max_blockio);
   pl->gz = alloc(max_z1 ? max_z1 : 16);
@@ -823,8 +826,10 @@ int run_forward(Ctx* c, const Plan& pl, const float* state_c, float* state_rs, c
   return RN18_OK;
 }
 
+// teacher: the list and its temperature and weight (a step of
+// rn18_train_step_distill), or NULL.
 int run_train(Ctx* c, const Plan& pl, float* state, const float* images, const int32_t* labels, float lr,
-              float* loss) {
+              float* loss, const DistillArgs* teacher = nullptr) {
   const Arch& a = c->arch;
   char* ws = (char*)c->ws;
   hipStream_t st = c->stream;
@@ -844,9 +849,24 @@ int run_train(Ctx* c, const Plan& pl, float* state, const float* images, const i
     TIMED(RN18_K_HEAD, 5, 0, "dropout_kernel", 0.0, 8.0 * N * F,
           dropout_launch(f, (long)N * F, c->drop_seed, c->drop_step, c->drop_thresh, c->drop_scale, st));
   TIMED(RN18_K_HEAD, 0, 0, "gemm_f32_kernel", fcf, 0.0, gemm_f32_launch(f, F, 1, state + a.fc_w, 1, F, state + a.fc_b, logits, N, C, F, hpart, st));
-  TIMED(RN18_K_HEAD, 1, 0, "softmax_ce_kernel", 0.0, 8.0 * N * C,
-        softmax_ce_launch(logits, labels, N, C, dlog, (float*)(ws + pl.rowloss),
-                          loss ? loss : (float*)(ws + pl.lossbuf), c->err, st, c->ls));
+  float* lossp = loss ? loss : (float*)(ws + pl.lossbuf);
+  if (teacher) {
+    DistillArgs t = *teacher;
+    t.z = logits;
+    t.labels = labels;
+    t.dz = dlog;
+    t.row_loss = (float*)(ws + pl.rowloss);
+    t.R = N;
+    t.ldz = t.lddz = t.C = C;
+    t.scale = 1.0f / (float)N;
+    t.err = c->err;
+    t.ls = c->ls;
+    TIMED(RN18_K_HEAD, 7, 0, "distill_row_kernel", 0.0, 8.0 * N * (C + t.K),
+          distill_launch(RN18_FP32, t, lossp, ws + pl.distill, st));
+  } else {
+    TIMED(RN18_K_HEAD, 1, 0, "softmax_ce_kernel", 0.0, 8.0 * N * C,
+          softmax_ce_launch(logits, labels, N, C, dlog, (float*)(ws + pl.rowloss), lossp, c->err, st, c->ls));
+  }
   // classifier backward: dW = dz^T f, db = sum dz, df = dz W
   TIMED(RN18_K_HEAD, 2, 0, "gemm_f32_kernel", fcf, 0.0, gemm_f32_launch(dlog, 1, C, f, F, 1, nullptr, grad + a.fc_w, C, F, N, hpart, st));
   TIMED(RN18_K_HEAD, 3, 0, "colsum_kernel", 0.0, 4.0 * N * C, colsum_launch(dlog, N, C, grad + a.fc_b, st));
@@ -1292,10 +1312,19 @@ int rn18_set_workspace(rn18_ctx* h, void* dev, size_t bytes) {
   return RN18_OK;
 }
 
-int rn18_train_step(rn18_ctx* h, float* state, const float* images, const int32_t* labels, int N, int H, int W,
-                    float lr, float* loss) {
+// The checks of a loss's temperature and mix.
+static int mix_check(float temperature, float alpha) {
+  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.0f / temperature))
+    return fail(RN18_EINVAL, "the temperature must be positive and finite");
+  if (!(alpha >= 0.f && alpha <= 1.f)) return fail(RN18_EINVAL, "alpha must be in [0, 1]");
+  return RN18_OK;
+}
+
+static int train_step(rn18_ctx* h, float* state, const float* images, const int32_t* labels, int N, int H, int W,
+                      float lr, float* loss, const DistillArgs* teacher) {
   if (!h) return fail(RN18_EINVAL, "ctx is NULL");
-  if (!state || !images || !labels) return fail(RN18_EINVAL, "state, images and labels must be non-NULL");
+  if (!state || !images || (!labels && !teacher))
+    return fail(RN18_EINVAL, "state, images and labels must be non-NULL");
   if (!aligned16(state) || !aligned16(images) || (loss && ((uintptr_t)loss & 3u)))
     return fail(RN18_EINVAL, "misaligned pointer");
   if (!isfinite(lr)) return fail(RN18_EINVAL, "lr is not finite");
@@ -1304,9 +1333,32 @@ int rn18_train_step(rn18_ctx* h, float* state, const float* images, const int32_
   int r = get_plan(&c, N, H, W, &pl);
   if (r) return r;
   if ((r = ensure_ws(&c, *pl))) return r;
-  if ((r = run_train(&c, *pl, state, images, labels, lr, loss))) return r;
+  if ((r = run_train(&c, *pl, state, images, labels, lr, loss, teacher))) return r;
   ++c.drop_step;
   return RN18_OK;
+}
+
+int rn18_train_step(rn18_ctx* h, float* state, const float* images, const int32_t* labels, int N, int H, int W,
+                    float lr, float* loss) {
+  return train_step(h, state, images, labels, N, H, W, lr, loss, nullptr);
+}
+
+int rn18_train_step_distill(rn18_ctx* h, float* state, const float* images, const int32_t* labels,
+                            const float* t_vals, const int32_t* t_idx, int K, float temperature, float alpha, int N,
+                            int H, int W, float lr, float* loss) {
+  if (!t_vals || !t_idx) return fail(RN18_EINVAL, "t_vals and t_idx must be non-NULL");
+  if (((uintptr_t)t_vals | (uintptr_t)t_idx | (uintptr_t)labels) & 3u) return fail(RN18_EINVAL, "misaligned pointer");
+  if (K < 1 || K > kTopMax) return fail(RN18_EINVAL, "K must be in [1, %d]", kTopMax);
+  const int r = mix_check(temperature, alpha);
+  if (r) return r;
+  if (!labels && alpha != 1.0f) return fail(RN18_EINVAL, "labels may be NULL for alpha = 1 only");
+  DistillArgs t{};
+  t.t_vals = t_vals;
+  t.t_idx = t_idx;
+  t.K = K;
+  t.temperature = temperature;
+  t.alpha = alpha;
+  return train_step(h, state, images, labels, N, H, W, lr, loss, &t);
 }
 
 int rn18_set_loss_scale(rn18_ctx* h, float scale, unsigned growth_interval) {
@@ -1836,9 +1888,7 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
       (r = words_check("labels", labels, false)) || (r = words_check("row_weight", row_weight, false)) ||
       (r = words_check("row_loss", row_loss, R > 0)) || (r = words_check("loss", loss, false)))
     return r;
-  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.0f / temperature))
-    return fail(RN18_EINVAL, "the temperature must be positive and finite");
-  if (!(alpha >= 0.f && alpha <= 1.f)) return fail(RN18_EINVAL, "alpha must be in [0, 1]");
+  if ((r = mix_check(temperature, alpha))) return r;
   if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
   if ((r = ws_check(ws, ws_bytes, distill_workspace(prec, R, C, K)))) return r;
   const DistillArgs a{z, t_vals, t_idx, labels, row_weight, dz, row_loss, R, ldz, lddz, C, K, temperature, alpha,

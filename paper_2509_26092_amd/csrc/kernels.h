@@ -302,8 +302,8 @@ struct DistillArgs {
   int C, K;
   float temperature, alpha, scale;
   // of a training step (both may be NULL): the context's sticky error flags,
-  // set for a label outside [0, C) or a class of the list that is neither in
-  // there nor -1, and its loss scale, a factor of dz
+  // set for a label or a listed class that is neither in [0, C) nor -1, and
+  // its loss scale, a factor of dz
   unsigned* err;
   const LossScale* ls;
 };
