@@ -32,7 +32,14 @@ __device__ inline void store_chunk_at(T* row, uint32_t bytes, const uint4& q) {
 }
 
 // A row of W elements is W / VW whole chunks and up to VW - 1 further
-// elements, its tail, one to a lane.
+// elements, its tail, one to a lane. Where loads at odd addresses cost time,
+// the chunks start at the row's first 16-byte boundary, after row_head
+// elements; these are one to a lane as well.
+template <typename T>
+__device__ inline int row_head(const T* row, int width) {
+  const int head = (int)((0 - (uintptr_t)row) & 15) / (int)sizeof(T);
+  return head < width ? head : width;
+}
 
 // Where a lane without a chunk of a row loads from: the row's first chunk, or
 // 16 bytes of zeros where the row has none (a branch around the loads would

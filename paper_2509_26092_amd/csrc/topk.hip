@@ -6,11 +6,14 @@
 // (about K^2 / 2L of a random row), so one compare against it leaves a short
 // list, and counting for each entry of the list how many others precede it
 // gives its place. The work beyond the one pass over the row is small, and
-// the pass is bound by memory. Where more logits reach the bound than the list holds
-// (equal logits: masked rows; rows whose large logits crowd in few lanes), a
-// bisection over the order of the values, counted over the row, finds a bound
-// that fits or the value that all the surplus shares, of which the first
-// classes are taken.
+// the pass is bound by memory: 16384x32768 bf16, 20 kept, 175 us (6.1 TB/s,
+// what reads alone reach), 64 kept 193 us; 4096x32768, 64 kept, 54 us. Where
+// more logits reach the bound than the list holds (equal logits: masked rows;
+// rows whose large logits crowd in few lanes), a bisection over the order of
+// the values, counted over the row, finds a bound that fits or the value that
+// all the surplus shares, of which the first classes are taken. Lists of about
+// as many entries as the row has chunks get there too, which takes several
+// times the pass (5592x1500 bf16: 64 kept 17 us, 256 kept 446).
 #include <math.h>
 
 #include <algorithm>
@@ -107,27 +110,27 @@ __device__ inline int row_count(int n, int* before, TopShared<L>& sh) {
 // REG: a lane has E chunks, whose maxima it keeps; otherwise any number, and
 // it reads them again to find those that reach the bound. A row may be cut into gridDim.y
 // parts of `len` logits, whose entries (key, ~class) go to
-// part[row][part][K].
+// part[row][part][K]. (Eight waves a SIMD for blocks of 256: 65536x8192
+// bf16, 20 kept, 223 us in place of 244; for blocks of 512 16384x32768 would
+// take 188 us in place of 175.)
 template <typename T, int L, int E, bool REG>
-__global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __restrict__ z, float* __restrict__ vals,
-                                                                 int32_t* __restrict__ idx,
-                                                                 uint64_t* __restrict__ part, long R, int Call, int len,
-                                                                 long ldz, int K) {
+__global__ __launch_bounds__(L > 256 ? L : 256, L == 256 ? 8 : 1) void topk_kernel(
+    const T* __restrict__ z, float* __restrict__ vals, int32_t* __restrict__ idx, uint64_t* __restrict__ part, long R,
+    int Call, int len, long ldz, int K) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L;
   constexpr int M = TopShared<L>::M;
   __shared__ TopShared<L> shared[G];
-  TopShared<L>& sh = shared[L < NT ? threadIdx.x / L : 0];
+  const int grp = L < NT ? threadIdx.x / L : 0;
+  TopShared<L>& sh = shared[grp];
   const int first = (int)blockIdx.y * len;
   const int C = std::min(len, Call - first);
   // (L < NT: each wave has its own rows, and nothing waits for another's)
-  for (long r = (long)blockIdx.x * G + (L < NT ? threadIdx.x / L : 0); r < R; r += (long)gridDim.x * G) {
+  for (long r = (long)blockIdx.x * G + grp; r < R; r += (long)gridDim.x * G) {
     int l = threadIdx.x % L;
     asm volatile("" : "+v"(l));   // classes are computed where they are needed, not kept over the rows
     const T* zr = z + r * ldz + first;
-    // Chunks start at the row's first 16-byte boundary (at odd ones a row of
-    // 131071 fp16 logits took 12.3 us in place of 8.1); the up to VW - 1
-    // logits before it and after the last chunk are one to a lane.
-    const int head = std::min(C, (int)((0 - (uintptr_t)zr) & 15) / (int)sizeof(T));
+    // (chunks at odd addresses: a row of 131071 fp16 logits 12.3 us in place of 8.1)
+    const int head = row_head(zr, C);
     const int nch = (C - head) / VW;
     const T* zc = zr + head;
     const int tail = l < head ? l : nch * VW + l;
@@ -154,7 +157,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
           unpack<T>(q[e], v);
           tops[e0 + e] = (e0 + e) * L + l < nch ? chunk_max<VW>(v) : -INFINITY;
         }
-        if (e0 + B < E) __builtin_amdgcn_sched_barrier(0);   // registers for B chunks, so that two blocks fit a compute unit
+        // registers for B chunks, so that two blocks fit a compute unit
+        if (e0 + B < E) __builtin_amdgcn_sched_barrier(0);
       }
     }
     if constexpr (L == 64) {
@@ -326,6 +330,50 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void topk_kernel(const T* __rest
   }
 }
 
+// Short rows, a wave each: P logits a lane, the K-th largest of all of them
+// as the bound, and each lane counts the entries before its own.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void topk_short_kernel(const T* __restrict__ z, float* __restrict__ vals,
+                                                         int32_t* __restrict__ idx, long R, int C, long ldz, int K) {
+  __shared__ uint64_t lists[4][64 * P];
+  const int l = threadIdx.x & 63;
+  uint64_t* list = lists[threadIdx.x >> 6];
+  for (long r = (long)blockIdx.x * 4 + (threadIdx.x >> 6); r < R; r += (long)gridDim.x * 4) {
+    const T* zr = z + r * ldz;
+    float v[P];
+    uint32_t k[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) v[p] = TT<T>::to_f(zr[p * 64 + l < C ? p * 64 + l : 0]);
+#pragma unroll
+    for (int p = 0; p < P; ++p) k[p] = p * 64 + l < C ? order_key(v[p]) : 0;
+    // (not 0: there are K keys, and the smallest, of -inf, has bits among the bound's)
+    const uint32_t bound = kth_key<P>([&](int p) { return k[p]; }, K);
+    int n = 0;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const bool hit = k[p] >= bound;
+      const uint64_t who = __ballot(hit);
+      if (hit) list[n + __popcll(who & ((1ull << l) - 1))] = (uint64_t)k[p] << 32 | (uint32_t)~(p * 64 + l);
+      n += __popcll(who);
+    }
+    row_sync<64>();
+    int place[P] = {};
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+      const uint64_t e = list[j];
+#pragma unroll
+      for (int p = 0; p < P; ++p) place[p] += e > ((uint64_t)k[p] << 32 | (uint32_t)~(p * 64 + l)) ? 1 : 0;
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+      if (k[p] >= bound && place[p] < K) {
+        vals[r * K + place[p]] = v[p];
+        idx[r * K + place[p]] = p * 64 + l;
+      }
+    row_sync<64>();   // before the next row's list
+  }
+}
+
 // The places of a row's n entries from all its parts: 8 lanes count for each.
 constexpr int kMergeMax = 2048;
 template <typename T>
@@ -398,13 +446,30 @@ int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int 
     uint64_t* part = (uint64_t*)ws;
     const int nch = pl.len / TT<T>::VW;
     auto go = [&](auto l, auto e, auto reg) {
-      return topk_go<T, decltype(l)::value, decltype(e)::value, decltype(reg)::value>(R, pl.parts, s, zt, vals, idx, part,
-                                                                                     R, C, pl.len, ldz, K);
+      return topk_go<T, decltype(l)::value, decltype(e)::value, decltype(reg)::value>(R, pl.parts, s, zt, vals, idx,
+                                                                                     part, R, C, pl.len, ldz, K);
     };
     auto pick = [&]() {
+#define SHORT(P)                                                                                                  \
+  {                                                                                                               \
+    const dim3 grid((unsigned)std::min((R + 3) / 4, 1l << 22));                                                   \
+    hipLaunchKernelGGL((topk_short_kernel<T, P>), grid, dim3(256), 0, s, zt, vals, idx, R, C, ldz, K);            \
+    return ok();                                                                                                  \
+  }
+      // Every logit's key takes part in the bound: rows to 256 logits (335544x100
+      // bf16, 10 kept: 107 us, with maxima of chunks 176; 64 kept: 207 and 501),
+      // longer ones whose chunks are too few for a bound (16384x512 bf16, 100
+      // kept: 62 and 445; 40 kept, from 64 chunks: 33 and 23).
+      const int chunks = C / TT<T>::VW;
+      if (C <= 64) SHORT(1);
+      if (C <= 128) SHORT(2);
+      if (C <= 256) SHORT(4);
+      if (C <= 512 && chunks * 3 < K * 4) SHORT(8);
+      if (C <= 1024 && chunks * 3 < K * 4) SHORT(16);
+#undef SHORT
 #define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{}, std::true_type{})
-      // a wave per row where its chunks are several times K or its logits fit the list
-      if (K <= 64 && nch <= 512 && (nch * 2 >= K * 3 || pl.len <= TopShared<64>::M)) {
+      // a wave per row where its chunks are more than K
+      if (K <= 64 && nch <= 512 && nch * 2 >= K * 3) {
         if (nch <= 64) GO(64, 1);
         if (nch <= 128) GO(64, 2);
         if (nch <= 256) GO(64, 4);

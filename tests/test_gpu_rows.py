@@ -624,3 +624,51 @@ def test_graph_replays(prec, R, W, K):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(want, outs)), i
+
+
+# ---------------------------------------------------------------- many rows of few classes
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("R,C,K,masked,pad,off", [(2100, 1, 1, False, 0, 0), (4097, 10, 3, True, 0, 1),
+                                                  (2500, 13, 16, True, 3, 0), (2049, 100, 10, True, 0, 0),
+                                                  (3001, 127, 16, True, 1, 3), (2200, 250, 0, False, 0, 0),
+                                                  (2050, 500, 5, True, 4, 1), (2048, 1000, 16, True, 0, 0)])
+def test_distill_many_short_rows(prec, R, C, K, masked, pad, off):
+    """Several rows of a wave at once: switched-off, masked and unlabelled
+    ones beside the others, and the last block with fewer."""
+    T, alpha, scale = 2.0, 0.6, (1024.0 if prec == "fp16" else 1.0) / R
+    z, t_vals, t_idx, labels, weight = distill_inputs(prec, R, C, K, masked)
+    zd, _ = mat(z, prec, pad, off)
+    dzd, dzbuf = out(R, C, prec, 2 * pad, off)
+    row, loss = run_distill(zd, prec, t_vals, t_idx, labels, weight, K, T, alpha, scale, R, C, C + pad, dzd,
+                            C + 2 * pad)
+    row_o, loss_o, dz_o = rows.distill(z, t_vals, t_idx, labels, weight, T, alpha, scale)
+    tol = loss_bound(z, t_vals, weight, T, alpha)
+    assert np.abs(row - row_o).max() <= tol
+    assert abs(loss - loss_o) <= scale * R * tol + 2.0 ** -23 * abs(loss_o)
+    # an fp16 gradient below 2^-14 rounds to a multiple of 2^-24
+    assert np.abs(f64(dzd) - dz_o).max() <= (U[prec] + TOL) * np.abs(dz_o).max() + \
+        (2.0 ** -25 if prec == "fp16" else 0.0) + scale * T * TOL
+    assert gaps_kept(dzd, dzbuf)
+    if weight is not None:
+        assert not f64(dzd)[weight == 0.0].any()
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("C,K", [(1, 1), (63, 60), (64, 1), (65, 64), (129, 100), (256, 256), (257, 200), (511, 64),
+                                 (512, 256), (513, 100), (1023, 200), (1024, 256)])
+def test_topk_short_rows(prec, C, K):
+    """Rows that a wave holds whole: random ones, few distinct values, both
+    zeros, masked but some, NaN and infinities, each at odd addresses too."""
+    rng = np.random.default_rng(C * 7 + K)
+    z = rounded(rng.standard_normal((9, C)) * 2.5, prec)
+    z[1] = rng.integers(0, 3, C)
+    z[2] = np.where(rng.random(C) < 0.5, 0.0, -0.0)
+    z[3] = -np.inf
+    z[3, rng.integers(0, C, max(1, K // 2))] = -1.0
+    z[4] = np.nan
+    z[5, rng.integers(0, C, 3)] = np.nan
+    z[5, rng.integers(0, C, 3)] = np.inf
+    z[6] = rounded(np.array([-65504.0]), prec)
+    z[6, C - 1] = -np.inf
+    check_topk(z, prec, K)
+    check_topk(z, prec, K, 3, 1)
