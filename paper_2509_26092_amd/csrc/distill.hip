@@ -7,7 +7,9 @@
 //
 // z is read once into registers, its maximum and sums of exponentials are
 // taken there, and dz is written from there: 4 bytes of traffic and two or
-// four exponentials an element in 16 bits. The few classes that the list or the
+// four exponentials an element in 16 bits. Bound by memory without labels
+// (16384x32768 bf16 457 us, 4.7 TB/s), with labels by memory and the vector
+// units together (10737x50001 bf16 454 us, without 415). The few classes that the list or the
 // label name are written a second time with their own terms, by the lane of
 // the first entry that names each. With sum q = 1 the soft term is
 // sum_k q_k (t'_k - z'_k) - log sum e^t' + log sum e^z' (t', z': over T, less
@@ -32,17 +34,21 @@ __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The teacher's list of a row and, as entry K, the label; the class of the
 // label is apart, and -1 fills the list's classes up to a multiple of 4.
+template <int KM>
 struct alignas(16) Entries {
-  int32_t cls[kTopMax];       // -1: not valid
-  float e[kTopMax + 1];       // t / T, then exp(t / T - their maximum)
-  float z[kTopMax + 1];       // the student's logit
+  int32_t cls[KM];       // -1: not valid
+  float e[KM + 1];       // t / T, then exp(t / T - their maximum)
+  float z[KM + 1];       // the student's logit
   int32_t label;
 };
+// Of rows whose lanes are part of a wave: an entry a lane.
+constexpr int kShortList = 16;
 
 // Loads a row's entries; zk: the student's logits of the entries, if they
 // have been gathered before, or NULL. Returns the largest t / T.
-template <typename T, int L, bool HARD>
-__device__ inline float load_entries(const DistillArgs& a, long r, int l, const T* zr, const float* zk, Entries& en) {
+template <typename T, int L, bool HARD, int KM>
+__device__ inline float load_entries(const DistillArgs& a, long r, int l, const T* zr, const float* zk,
+                                     Entries<KM>& en) {
   const float invt = 1.0f / a.temperature;
   float tm = -INFINITY;
   bool bad = false;
@@ -79,8 +85,8 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
 // e (t' - z') over the entries.
 enum { SUM_T, SUM_1, SUM_Q, SUM_QD, SUMS };
 
-template <int L>
-__device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, Entries& en, float* s) {
+template <int L, int KM>
+__device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, Entries<KM>& en, float* s) {
   const float invt = 1.0f / a.temperature;
   for (int k = l; k < a.K; k += L) {
     const float t = en.e[k] - tm, e = en.cls[k] < 0 ? 0.f : exp2_hw(t * kLog2e);
@@ -127,11 +133,11 @@ __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* 
   return w * v;
 }
 
-// The gradients of the classes [c0, c1) that entries name, each by the lane
-// of the first entry that names it.
-template <typename T, int L, bool HARD>
-__device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries& en, T* dr, int c0,
-                                     int c1) {
+// The gradients of the classes [c0, c1) and [0, head) that entries name, each
+// by the lane of the first entry that names it.
+template <typename T, int L, bool HARD, int KM>
+__device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries<KM>& en, T* dr, int c0,
+                                     int c1, int head) {
   for (int k = l; k < a.K + HARD; k += L) {
     const int at = k < a.K ? en.cls[k] : en.label;
     // entries of the same class, itself among them: most lists have none
@@ -140,7 +146,7 @@ __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad&
       const int4 c = *(const int4*)(en.cls + j);
       same += (c.x == at ? 1 : 0) + (c.y == at ? 1 : 0) + (c.z == at ? 1 : 0) + (c.w == at ? 1 : 0);
     }
-    if (at < c0 || at >= c1) continue;
+    if (at < 0 || (at >= head && (at < c0 || at >= c1))) continue;
     float q = k < a.K ? en.e[k] : 0.f;
     if (same > (k < a.K ? 1 : 0)) {
       bool first = true;
@@ -159,33 +165,37 @@ __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad&
   }
 }
 
-// One row in the registers of L lanes, E chunks each and a tail.
+// One row in the registers of L lanes, E chunks each; the elements before the
+// first chunk and after the last are one to a lane. (Chunks at the row's own
+// address, which an odd class count leaves unaligned: 10737x50001 bf16 528 us
+// in place of 415.)
 template <typename T, int L, int E, bool HARD>
 __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillArgs a) {
-  constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L;
-  __shared__ Entries entries[G];
+  constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L, KM = L < 64 ? kShortList : kTopMax;
+  __shared__ Entries<KM> entries[G];
   __shared__ float shm[L > 64 ? L / 64 : 1][2], shs[L > 64 ? L / 64 : 1][SUMS];
   const int grp = L < NT ? threadIdx.x / L : 0;
-  Entries& en = entries[grp];
-  const int nch = a.C / VW;
-  // (L < NT: each wave has its own rows, and nothing waits for another's)
+  Entries<KM>& en = entries[grp];
+  // (L < NT: a wave or part of one has its own rows, and nothing waits for
+  // another's; the lanes of a row leave the loop and skip a row together)
   for (long r = (long)blockIdx.x * G + grp; r < a.R; r += (long)gridDim.x * G) {
     int l = threadIdx.x % L;
     asm volatile("" : "+v"(l));   // offsets are computed where they are needed, not kept over the rows
     const T* zr = (const T*)a.z + r * a.ldz;
     T* dr = a.dz ? (T*)a.dz + r * a.lddz : nullptr;
-    const int tail = nch * VW + l;
+    const int head = row_head(zr, a.C), nch = (a.C - head) / VW;
+    const int tail = l < head ? l : nch * VW + l;
     const float w = a.weight ? a.weight[r] : 1.0f;
     if (w == 0.f) {   // the row may hold anything: not read
       if (l == 0) a.row_loss[r] = 0.f;
       if (dr) {
-        for (int c = l; c < nch; c += L) store_chunk(dr + c * VW, make_uint4(0, 0, 0, 0));
+        for (int c = l; c < nch; c += L) store_chunk(dr + head + c * VW, make_uint4(0, 0, 0, 0));
         if (tail < a.C) dr[tail] = TT<T>::from_f(0.f);
       }
       continue;
     }
     uint4 q[E];
-    const T* zc = chunk_base(zr, nch);
+    const T* zc = chunk_base(zr + head, nch);
 #pragma unroll
     for (int e = 0; e < E; ++e) q[e] = load_chunk_at(zc, (e * L + l < nch ? e * L + l : 0) * 16u);
     const float zt = tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
@@ -217,10 +227,10 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
       opaque(q[e]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (L == 64) row_sync<L>();
+    if (L <= 64) row_sync<L>();
     entry_sums<L>(a, l, tm, m, en, s);
     row_red<L>(s, shs, Sum());
-    if (L == 64) row_sync<L>();
+    if (L <= 64) row_sync<L>();
     const bool labelled = HARD && en.label >= 0;
     if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, HARD ? en.z[a.K] : 0.f, labelled);
     if (dr) {
@@ -231,12 +241,12 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
         unpack<T>(q[e], v);
 #pragma unroll
         for (int j = 0; j < VW; ++j) v[j] = grad_at<HARD>(g, v[j]);
-        if (e * L + l < nch) store_chunk_at(dr, (e * L + l) * 16u, pack<T>(v));
+        if (e * L + l < nch) store_chunk_at(dr + head, (e * L + l) * 16u, pack<T>(v));
         __builtin_amdgcn_sched_barrier(0);
       }
       if (tail < a.C) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, zt));
       row_sync<L>();   // the named classes are written after the rest
-      write_entries<T, L, HARD>(a, l, g, en, dr, 0, a.C);
+      write_entries<T, L, HARD>(a, l, g, en, dr, 0, a.C, 0);
     }
     row_sync<L>();   // before the next row's entries
   }
@@ -257,21 +267,22 @@ constexpr int kPartE = 4;   // chunks of a lane in flight
 template <typename T, bool HARD>
 __global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, Parts ps) {
   constexpr int VW = TT<T>::VW, L = 256;
-  __shared__ Entries en;
+  __shared__ Entries<kTopMax> en;
   __shared__ float shm[L / 64][1], shs[L / 64][2];
-  const int l = threadIdx.x, nch = a.C / VW;
-  const int c0 = (int)blockIdx.x * ps.chunks, c1 = std::min(nch, c0 + ps.chunks);
+  const int l = threadIdx.x, c0 = (int)blockIdx.x * ps.chunks;
   const bool last = (int)blockIdx.x == ps.n - 1;
   const float ct = kLog2e / a.temperature;
   for (long r = blockIdx.y; r < a.R; r += gridDim.y) {
     if (a.weight && a.weight[r] == 0.f) continue;
     const T* zr = (const T*)a.z + r * a.ldz;
+    const int head = row_head(zr, a.C), nch = (a.C - head) / VW, c1 = std::min(nch, c0 + ps.chunks);
+    const T* zc = zr + head;
     float* wr = ps.ws + r * ps.row_floats(a.K);
     if (blockIdx.x == 0) {
       load_entries<T, L, HARD>(a, r, l, zr, nullptr, en);
       for (int k = l; k < a.K + HARD; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
     }
-    const int tail = nch * VW + l;
+    const int tail = l < head ? l : nch * VW + l;   // (the last part has the head too)
     // a running maximum of the lane, and its sums relative to it
     float m = last && tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
     float s[2] = {m == -INFINITY ? 0.f : 1.f, HARD && m != -INFINITY ? 1.f : 0.f};
@@ -280,7 +291,7 @@ __global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, 
       uint4 q[kPartE];
       float v[kPartE][VW], top = m;
 #pragma unroll
-      for (int e = 0; e < kPartE; ++e) q[e] = load_chunk(zr + (long)std::min(b + e * L, c1 - 1) * VW);
+      for (int e = 0; e < kPartE; ++e) q[e] = load_chunk(zc + (long)std::min(b + e * L, c1 - 1) * VW);
 #pragma unroll
       for (int e = 0; e < kPartE; ++e) {
         unpack<T>(q[e], v[e]);
@@ -321,21 +332,21 @@ __global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, 
 template <typename T, bool HARD>
 __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, Parts ps) {
   constexpr int VW = TT<T>::VW, L = 256;
-  __shared__ Entries en;
+  __shared__ Entries<kTopMax> en;
   __shared__ float shm[L / 64][2], shs[L / 64][SUMS];
-  const int l = threadIdx.x, nch = a.C / VW;
-  const int c0 = (int)blockIdx.x * ps.chunks, c1 = std::min(nch, c0 + ps.chunks);
+  const int l = threadIdx.x, c0 = (int)blockIdx.x * ps.chunks;
   const bool last = (int)blockIdx.x == ps.n - 1;
   const float ct = kLog2e / a.temperature;
   for (long r = blockIdx.y; r < a.R; r += gridDim.y) {
     const T* zr = (const T*)a.z + r * a.ldz;
     T* dr = a.dz ? (T*)a.dz + r * a.lddz : nullptr;
+    const int head = row_head(zr, a.C), nch = (a.C - head) / VW, c1 = std::min(nch, c0 + ps.chunks);
     const float w = a.weight ? a.weight[r] : 1.0f;
-    const int tail = last && nch * VW + l < a.C ? nch * VW + l : -1;
+    const int mine = l < head ? l : nch * VW + l, tail = last && mine < a.C ? mine : -1;
     if (w == 0.f) {
       if (blockIdx.x == 0 && l == 0) a.row_loss[r] = 0.f;
       if (dr) {
-        for (int c = c0 + l; c < c1; c += L) store_chunk(dr + (long)c * VW, make_uint4(0, 0, 0, 0));
+        for (int c = c0 + l; c < c1; c += L) store_chunk(dr + head + (long)c * VW, make_uint4(0, 0, 0, 0));
         if (tail >= 0) dr[tail] = TT<T>::from_f(0.f);
       }
       continue;
@@ -362,7 +373,7 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
         uint4 q[kPartE];
 #pragma unroll
         for (int e = 0; e < kPartE; ++e)
-          if (b + e * L < c1) q[e] = load_chunk(zr + (long)(b + e * L) * VW);
+          if (b + e * L < c1) q[e] = load_chunk(zr + head + (long)(b + e * L) * VW);
 #pragma unroll
         for (int e = 0; e < kPartE; ++e)
           if (b + e * L < c1) {
@@ -370,12 +381,12 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
             unpack<T>(q[e], v);
 #pragma unroll
             for (int j = 0; j < VW; ++j) v[j] = grad_at<HARD>(g, v[j]);
-            store_chunk(dr + (long)(b + e * L) * VW, pack<T>(v));
+            store_chunk(dr + head + (long)(b + e * L) * VW, pack<T>(v));
           }
       }
       if (tail >= 0) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, TT<T>::to_f(zr[tail])));
       __syncthreads();   // the named classes are written after the rest
-      write_entries<T, L, HARD>(a, l, g, en, dr, c0 * VW, last ? a.C : c1 * VW);
+      write_entries<T, L, HARD>(a, l, g, en, dr, head + c0 * VW, last ? a.C : head + c1 * VW, last ? head : 0);
     }
     __syncthreads();
   }
@@ -436,6 +447,14 @@ int distill_go(const DistillArgs& a, const Parts& ps, hipStream_t s) {
     return ok();
   };
 #define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{})
+  // Many short rows with short lists: sixteen lanes a row, so that four rows
+  // share what a wave spends on sums and entries (335544x100 bf16, 10 kept:
+  // 75 us, with a wave a row 231; 67108x500: 39 and 52, 64 kept: 130 and 113).
+  if (nch <= 64 && a.K + HARD <= kShortList && a.R >= 8l * plan_cus()) {
+    if (nch <= 16) GO(16, 1);
+    if (nch <= 32) GO(16, 2);
+    GO(16, 4);
+  }
   if (nch <= 512 && a.R >= 4l * plan_cus()) {
     if (nch <= 64) GO(64, 1);
     if (nch <= 128) GO(64, 2);
