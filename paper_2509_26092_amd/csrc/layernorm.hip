@@ -10,7 +10,11 @@
 // sums are taken there (the mean first, then the squares of what is left of
 // it, so that a large mean costs no precision), and the result is written
 // from there. L lanes hold a row in E chunks of 16 bytes each: part of a
-// wave, a wave, or a block.
+// wave, a wave, or a block. On 802816x64 bf16 the forward pass takes 41 us and
+// the backward pass 60 (5.0 and 5.1 TB/s, a copy's rate), the backward pass on
+// 16384x8192 bf16 160 us (5.0 TB/s). Rows beyond a block's registers are read
+// two or three times: 4096x32768 bf16 forward 153 us (3.5 TB/s for one read
+// and one write), backward 358.
 #include <math.h>
 
 #include <algorithm>
@@ -813,7 +817,8 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
       const T *dyt = (const T*)dy, *xt = (const T*)x;
       T* dxt = (T*)dx;
       if (path == LN_TILE)
-        return bwd_tile<T>(L, E, small ? grid + ceil_div(D, 32) : grid, s, dyt, xt, gamma, mean, rstd, dxt, po, R, D, lddy, ldx, lddx);
+        return bwd_tile<T>(L, E, small ? grid + ceil_div(D, 32) : grid, s, dyt, xt, gamma, mean, rstd, dxt, po, R, D,
+                           lddy, ldx, lddx);
       if (path == LN_SHORT) {
         hipLaunchKernelGGL(ln_bwd_short_kernel<T>, dim3(grid), dim3(256), 0, s, dyt, xt, gamma, mean, rstd, dxt, po, R,
                            D, lddy, ldx, lddx);
