@@ -32,51 +32,76 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // 2^x by the hardware's instruction (1 ulp; 0 below 2^-126)
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The teacher's list of a row and, as entry K, the label; the class of the
-// label is apart, and -1 fills the list's classes up to a multiple of 4.
+// The teacher's list of a row; -1 fills its classes up to a multiple of 4.
 template <int KM>
 struct alignas(16) Entries {
-  int32_t cls[KM];       // -1: not valid
-  float e[KM + 1];       // t / T, then exp(t / T - their maximum)
-  float z[KM + 1];       // the student's logit
-  int32_t label;
+  int32_t cls[KM];   // -1: not valid
+  float e[KM];       // t / T, then exp(t / T - their maximum)
+  float z[KM];       // the student's logit
+  int32_t named;     // the label is one of the classes
 };
-// Of rows whose lanes are part of a wave: an entry a lane.
-constexpr int kShortList = 16;
+// Of rows whose lanes are part of a wave: lists that sixteen rows of a block
+// have room for.
+constexpr int kShortList = 64;
 
-// Loads a row's entries; zk: the student's logits of the entries, if they
-// have been gathered before, or NULL. Returns the largest t / T.
-template <typename T, int L, bool HARD, int KM>
-__device__ inline float load_entries(const DistillArgs& a, long r, int l, const T* zr, const float* zk,
-                                     Entries<KM>& en) {
+// What can be loaded of a row's entries and label before the student's logits
+// there: in flight ahead of the row's own chunks, it does not wait for them
+// (4096x32768 bf16 115 -> 111 us, 16777x1000 27.1 -> 25.2, 64 listed).
+struct First {
+  int i, label;
+  float t;
+};
+template <bool HARD>
+__device__ inline First load_first(const DistillArgs& a, long r, int l) {
+  First f = {-1, -1, -INFINITY};
+  if (HARD) f.label = a.labels[r];
+  if (l < a.K) {
+    f.i = a.t_idx[r * a.K + l];
+    f.t = a.t_vals[r * a.K + l];
+  }
+  return f;
+}
+
+// A row's label and the student's logit there; every lane holds them. (As an
+// entry after the others it cost lists of 64 a second round of every loop:
+// 16777x1000 bf16 40.0 us in place of 31.3.)
+struct Label {
+  int cls;   // -1: none
+  float z;
+};
+// zk: the student's logits of the K entries and the label, if they have been
+// gathered before, or NULL.
+template <typename T, bool HARD>
+__device__ inline Label load_label(const DistillArgs& a, int l, const First& f, const T* zr, const float* zk) {
+  if (!HARD) return {-1, 0.f};
+  const int i = f.label;
+  if (i >= 0 && i < a.C) return {i, zk ? zk[a.K] : TT<T>::to_f(zr[i])};
+  if (a.err && i != -1 && l == 0) atomicOr(a.err, (unsigned)DEVERR_LABEL);
+  return {-1, 0.f};
+}
+
+// Loads a row's entries. Returns the largest t / T.
+template <typename T, int L, int KM>
+__device__ inline float load_entries(const DistillArgs& a, long r, int l, const First& f, const T* zr,
+                                     const float* zk, Entries<KM>& en) {
   const float invt = 1.0f / a.temperature;
   float tm = -INFINITY;
   bool bad = false;
-  for (int k = l; k < a.K + HARD; k += L) {   // (the label last)
-    float t = -INFINITY;
-    int i = -1;
-    if (k < a.K) {
-      i = a.t_idx[r * a.K + k];
-      t = a.t_vals[r * a.K + k] * invt;
-      bad |= i < -1 || i >= a.C;
-      if (i < 0 || i >= a.C || t == -INFINITY || a.alpha == 0.f) {
-        i = -1;
-        t = -INFINITY;
-      }
-    } else {
-      i = a.labels[r];
-      if (i < 0 || i >= a.C) {
-        bad |= i != -1;
-        i = -1;
-      }
+  for (int k = l; k < a.K; k += L) {
+    int i = k == l ? f.i : a.t_idx[r * a.K + k];
+    float t = (k == l ? f.t : a.t_vals[r * a.K + k]) * invt;
+    bad |= i < -1 || i >= a.C;
+    if (i < 0 || i >= a.C || t == -INFINITY || a.alpha == 0.f) {
+      i = -1;
+      t = -INFINITY;
     }
-    if (k < a.K) en.cls[k] = i;
-    else en.label = i;
+    en.cls[k] = i;
     en.e[k] = t;
     en.z[k] = i < 0 ? 0.f : zk ? zk[k] : TT<T>::to_f(zr[i]);
     tm = max2(tm, t);
   }
   if (l < ((4 - (a.K & 3)) & 3)) en.cls[a.K + l] = -1;
+  if (l == 0) en.named = 0;
   if (a.err && bad) atomicOr(a.err, (unsigned)DEVERR_LABEL);
   return tm;
 }
@@ -86,12 +111,14 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
 enum { SUM_T, SUM_1, SUM_Q, SUM_QD, SUMS };
 
 template <int L, int KM>
-__device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, Entries<KM>& en, float* s) {
+__device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, const Label& lab,
+                                  Entries<KM>& en, float* s) {
   const float invt = 1.0f / a.temperature;
   for (int k = l; k < a.K; k += L) {
     const float t = en.e[k] - tm, e = en.cls[k] < 0 ? 0.f : exp2_hw(t * kLog2e);
     en.e[k] = e;
     s[SUM_Q] += e;
+    if (en.cls[k] >= 0 && en.cls[k] == lab.cls) en.named = 1;
     if (e != 0.f) s[SUM_QD] += e * (t - (en.z[k] - m) * invt);
   }
 }
@@ -134,21 +161,22 @@ __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* 
 }
 
 // The gradients of the classes [c0, c1) and [0, head) that entries name, each
-// by the lane of the first entry that names it.
+// by the lane of the first entry that names it, and of the label.
 template <typename T, int L, bool HARD, int KM>
-__device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Entries<KM>& en, T* dr, int c0,
-                                     int c1, int head) {
-  for (int k = l; k < a.K + HARD; k += L) {
-    const int at = k < a.K ? en.cls[k] : en.label;
+__device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad& g, const Label& lab,
+                                     const Entries<KM>& en, T* dr, int c0, int c1, int head) {
+  auto outside = [&](int at) { return at < 0 || (at >= head && (at < c0 || at >= c1)); };
+  for (int k = l; k < a.K; k += L) {
+    const int at = en.cls[k];
     // entries of the same class, itself among them: most lists have none
     int same = 0;
     for (int j = 0; j < a.K; j += 4) {
       const int4 c = *(const int4*)(en.cls + j);
       same += (c.x == at ? 1 : 0) + (c.y == at ? 1 : 0) + (c.z == at ? 1 : 0) + (c.w == at ? 1 : 0);
     }
-    if (at < 0 || (at >= head && (at < c0 || at >= c1))) continue;
-    float q = k < a.K ? en.e[k] : 0.f;
-    if (same > (k < a.K ? 1 : 0)) {
+    if (outside(at)) continue;
+    float q = en.e[k];
+    if (same > 1) {
       bool first = true;
       q = 0.f;
       for (int j = 0; j < a.K; ++j)
@@ -160,9 +188,11 @@ __device__ inline void write_entries(const DistillArgs& a, int l, const RowGrad&
     }
     float v = grad_at<HARD>(g, en.z[k]);
     if (g.fq != 0.f) v -= g.fq * q;   // (a row without a soft term: q may be anything)
-    if (HARD && at == en.label) v -= g.fh;
+    if (HARD && at == lab.cls) v -= g.fh;
     dr[at] = TT<T>::from_f(v);
   }
+  if (HARD && l == L - 1 && !outside(lab.cls) && !en.named)
+    dr[lab.cls] = TT<T>::from_f(grad_at<HARD>(g, lab.z) - g.fh);
 }
 
 // One row in the registers of L lanes, E chunks each; the elements before the
@@ -194,12 +224,14 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
       }
       continue;
     }
+    const First first = load_first<HARD>(a, r, l);
     uint4 q[E];
     const T* zc = chunk_base(zr + head, nch);
 #pragma unroll
     for (int e = 0; e < E; ++e) q[e] = load_chunk_at(zc, (e * L + l < nch ? e * L + l : 0) * 16u);
     const float zt = tail < a.C ? TT<T>::to_f(zr[tail]) : -INFINITY;
-    float mx[2] = {zt, load_entries<T, L, HARD>(a, r, l, zr, nullptr, en)};
+    const Label lab = load_label<T, HARD>(a, l, first, zr, nullptr);
+    float mx[2] = {zt, load_entries<T, L>(a, r, l, first, zr, nullptr, en)};
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       float v[VW];
@@ -228,11 +260,11 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
       __builtin_amdgcn_sched_barrier(0);
     }
     if (L <= 64) row_sync<L>();
-    entry_sums<L>(a, l, tm, m, en, s);
+    entry_sums<L>(a, l, tm, m, lab, en, s);
     row_red<L>(s, shs, Sum());
     if (L <= 64) row_sync<L>();
-    const bool labelled = HARD && en.label >= 0;
-    if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, HARD ? en.z[a.K] : 0.f, labelled);
+    const bool labelled = lab.cls >= 0;
+    if (l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, lab.z, labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
 #pragma unroll
@@ -246,7 +278,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void distill_row_kernel(DistillA
       }
       if (tail < a.C) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, zt));
       row_sync<L>();   // the named classes are written after the rest
-      write_entries<T, L, HARD>(a, l, g, en, dr, 0, a.C, 0);
+      write_entries<T, L, HARD>(a, l, g, lab, en, dr, 0, a.C, 0);
     }
     row_sync<L>();   // before the next row's entries
   }
@@ -279,8 +311,11 @@ __global__ __launch_bounds__(256) void distill_part_stats_kernel(DistillArgs a, 
     const T* zc = zr + head;
     float* wr = ps.ws + r * ps.row_floats(a.K);
     if (blockIdx.x == 0) {
-      load_entries<T, L, HARD>(a, r, l, zr, nullptr, en);
-      for (int k = l; k < a.K + HARD; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
+      const First first = load_first<HARD>(a, r, l);
+      load_entries<T, L>(a, r, l, first, zr, nullptr, en);
+      for (int k = l; k < a.K; k += L) wr[4 * ps.n + k] = en.z[k];   // the lane's own entries
+      const Label lab = load_label<T, HARD>(a, l, first, zr, nullptr);
+      if (HARD && l == 0) wr[4 * ps.n + a.K] = lab.z;
     }
     const int tail = l < head ? l : nch * VW + l;   // (the last part has the head too)
     // a running maximum of the lane, and its sums relative to it
@@ -352,7 +387,9 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
       continue;
     }
     const float* wr = ps.ws + r * ps.row_floats(a.K);
-    float mx[2] = {-INFINITY, load_entries<T, L, HARD>(a, r, l, zr, wr + 4 * ps.n, en)};
+    const First first = load_first<HARD>(a, r, l);
+    const Label lab = load_label<T, HARD>(a, l, first, zr, wr + 4 * ps.n);
+    float mx[2] = {-INFINITY, load_entries<T, L>(a, r, l, first, zr, wr + 4 * ps.n, en)};
     for (int p = l; p < ps.n; p += L) mx[0] = max2(mx[0], wr[4 * p]);
     row_red<L>(mx, shm, Max());
     const float m = mx[0] == -INFINITY ? 0.f : mx[0], tm = mx[1] == -INFINITY ? 0.f : mx[1];
@@ -363,10 +400,10 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
       s[SUM_T] += wr[4 * p + 1] * exp2_hw((mp - m) * ct);
       if (HARD) s[SUM_1] += wr[4 * p + 2] * exp2_hw((mp - m) * kLog2e);
     }
-    entry_sums<L>(a, l, tm, m, en, s);
+    entry_sums<L>(a, l, tm, m, lab, en, s);
     row_red<L>(s, shs, Sum());
-    const bool labelled = HARD && en.label >= 0;
-    if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, HARD ? en.z[a.K] : 0.f, labelled);
+    const bool labelled = lab.cls >= 0;
+    if (blockIdx.x == 0 && l == 0) a.row_loss[r] = row_loss_of<HARD>(a, w, s, m, lab.z, labelled);
     if (dr) {
       const RowGrad g = row_grad<HARD>(a, w, m, s, labelled);
       for (int b = c0 + l; b < c1; b += L * kPartE) {
@@ -386,7 +423,7 @@ __global__ __launch_bounds__(256) void distill_part_grad_kernel(DistillArgs a, P
       }
       if (tail >= 0) dr[tail] = TT<T>::from_f(grad_at<HARD>(g, TT<T>::to_f(zr[tail])));
       __syncthreads();   // the named classes are written after the rest
-      write_entries<T, L, HARD>(a, l, g, en, dr, head + c0 * VW, last ? a.C : head + c1 * VW, last ? head : 0);
+      write_entries<T, L, HARD>(a, l, g, lab, en, dr, head + c0 * VW, last ? a.C : head + c1 * VW, last ? head : 0);
     }
     __syncthreads();
   }
@@ -447,10 +484,12 @@ int distill_go(const DistillArgs& a, const Parts& ps, hipStream_t s) {
     return ok();
   };
 #define GO(L, E) return go(std::integral_constant<int, L>{}, std::integral_constant<int, E>{})
-  // Many short rows with short lists: sixteen lanes a row, so that four rows
-  // share what a wave spends on sums and entries (335544x100 bf16, 10 kept:
-  // 75 us, with a wave a row 231; 67108x500: 39 and 52, 64 kept: 130 and 113).
-  if (nch <= 64 && a.K + HARD <= kShortList && a.R >= 8l * plan_cus()) {
+  // Many short rows: sixteen lanes a row, so that four rows share what a wave
+  // spends on sums and entries, unless entries are most of the work
+  // (167772x100 bf16, 20 listed: 49 us, with a wave a row 119; 64 listed: 88
+  // and 140; 55924x300: 46 and 53; 33554x500, 20 listed: 26 and 31, 64: 45
+  // and 36).
+  if (nch <= 64 && a.K <= kShortList && nch * a.K <= 2400 && a.R >= 8l * plan_cus()) {
     if (nch <= 16) GO(16, 1);
     if (nch <= 32) GO(16, 2);
     GO(16, 4);
