@@ -8,10 +8,11 @@
 // z is read once into registers, its maximum and sums of exponentials are
 // taken there, and dz is written from there: 4 bytes of traffic and two or
 // four exponentials an element in 16 bits. Bound by memory without labels
-// (16384x32768 bf16 457 us, 4.7 TB/s), with labels by memory and the vector
-// units together (10737x50001 bf16 454 us, without 415). The few classes that the list or the
-// label name are written a second time with their own terms, by the lane of
-// the first entry that names each. With sum q = 1 the soft term is
+// (16384x32768 bf16, 64 listed, 449 us, 4.8 TB/s), with labels by memory and
+// the vector units together (4096x131071 bf16 585 us, without 475). The few
+// classes that the list or the label name are written a second time with
+// their own terms, by the lane of the first entry that names each. With
+// sum q = 1 the soft term is
 // sum_k q_k (t'_k - z'_k) - log sum e^t' + log sum e^z' (t', z': over T, less
 // their maxima), so that every sum of a row is taken in one step.
 #include <math.h>
