@@ -399,12 +399,15 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, 
 // Columns of the partial rows added up in a fixed order: 8 lanes of 4 columns
 // by 128 groups of rows a block (short chains of loads, and most of the time
 // of this kernel is their latency), then the groups' sums by fours and the
-// fours in order.
+// fours in order. One launch takes up to kSumCols columns from c0 on: its
+// threads are counted in 32 bits, which 2^27 columns would pass.
+constexpr int kSumCols = 1 << 26;
 __global__ __launch_bounds__(1024) void ln_param_sum_kernel(const float* __restrict__ part, int nb, int D, int Dp,
-                                                            float* __restrict__ dgamma, float* __restrict__ dbeta) {
+                                                            int c0, float* __restrict__ dgamma,
+                                                            float* __restrict__ dbeta) {
   __shared__ float sh[128][33], sh2[32][33];
   const int cl = threadIdx.x & 7, rg = threadIdx.x >> 3;
-  const int c = blockIdx.x * 32 + cl * 4;
+  const int c = c0 + blockIdx.x * 32 + cl * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < Dp) {
     const float* p = part + (long)blockIdx.y * Dp + c;
@@ -419,7 +422,7 @@ __global__ __launch_bounds__(1024) void ln_param_sum_kernel(const float* __restr
   const int k = threadIdx.x & 31, g = threadIdx.x >> 5;
   sh2[g][k] = (sh[4 * g][k] + sh[4 * g + 1][k]) + (sh[4 * g + 2][k] + sh[4 * g + 3][k]);
   __syncthreads();
-  const int col = blockIdx.x * 32 + k;
+  const int col = c0 + blockIdx.x * 32 + k;
   float* o = blockIdx.y ? dbeta : dgamma;
   if (g == 0 && col < D && o) {
     float t = sh2[0][k];
@@ -833,11 +836,13 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
     });
     if (r) return r;
   }
-  if (params && !small) {
-    hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(po.Dp, 32), 2), dim3(1024), 0, s, (const float*)ws, grid, D,
-                       po.Dp, dgamma, dbeta);
-    return ok();
-  }
+  if (params && !small)
+    for (int c0 = 0; c0 < po.Dp; c0 += kSumCols) {
+      hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(std::min(po.Dp - c0, kSumCols), 32), 2), dim3(1024), 0, s,
+                         (const float*)ws, grid, D, po.Dp, c0, dgamma, dbeta);
+      const int r = ok();
+      if (r) return r;
+    }
   return 0;
 }
 
