@@ -13,8 +13,11 @@
 // classes that the list or the label name are written a second time with
 // their own terms, by the lane of the first entry that names each. With
 // sum q = 1 the soft term is
-// sum_k q_k (t'_k - z'_k) - log sum e^t' + log sum e^z' (t', z': over T, less
-// their maxima), so that every sum of a row is taken in one step.
+// alpha T (sum_k q_k (t_k - z_k) + T (log sum e^z' - log sum e^t')), t and z
+// less their maxima, t' and z' over T too, so that every sum of a row is taken
+// in one step. The maxima are taken out before the division by T and the
+// sum over the entries is multiplied by T once: no quotient by a small T, nor T^2,
+// leaves fp32's range on the way.
 #include <math.h>
 
 #include <algorithm>
@@ -37,7 +40,7 @@ __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 template <int KM>
 struct alignas(16) Entries {
   int32_t cls[KM];   // -1: not valid
-  float e[KM];       // t / T, then exp(t / T - their maximum)
+  float e[KM];       // t, then exp((t - the largest t) / T)
   float z[KM];       // the student's logit
   int32_t named;     // the label is one of the classes
 };
@@ -81,16 +84,15 @@ __device__ inline Label load_label(const DistillArgs& a, int l, const First& f, 
   return {-1, 0.f};
 }
 
-// Loads a row's entries. Returns the largest t / T.
+// Loads a row's entries. Returns the largest t.
 template <typename T, int L, int KM>
 __device__ inline float load_entries(const DistillArgs& a, long r, int l, const First& f, const T* zr,
                                      const float* zk, Entries<KM>& en) {
-  const float invt = 1.0f / a.temperature;
   float tm = -INFINITY;
   bool bad = false;
   for (int k = l; k < a.K; k += L) {
     int i = k == l ? f.i : a.t_idx[r * a.K + k];
-    float t = (k == l ? f.t : a.t_vals[r * a.K + k]) * invt;
+    float t = k == l ? f.t : a.t_vals[r * a.K + k];
     bad |= i < -1 || i >= a.C;
     if (i < 0 || i >= a.C || t == -INFINITY || a.alpha == 0.f) {
       i = -1;
@@ -108,19 +110,19 @@ __device__ inline float load_entries(const DistillArgs& a, long r, int l, const 
 }
 
 // A row's sums: of exp(z') and exp(z - m) over the classes, of e and of
-// e (t' - z') over the entries.
+// e (t - z) over the entries.
 enum { SUM_T, SUM_1, SUM_Q, SUM_QD, SUMS };
 
 template <int L, int KM>
 __device__ inline void entry_sums(const DistillArgs& a, int l, float tm, float m, const Label& lab,
                                   Entries<KM>& en, float* s) {
-  const float invt = 1.0f / a.temperature;
+  const float ct = kLog2e / a.temperature;
   for (int k = l; k < a.K; k += L) {
-    const float t = en.e[k] - tm, e = en.cls[k] < 0 ? 0.f : exp2_hw(t * kLog2e);
+    const float t = en.e[k] - tm, e = en.cls[k] < 0 ? 0.f : exp2_hw(t * ct);
     en.e[k] = e;
     s[SUM_Q] += e;
     if (en.cls[k] >= 0 && en.cls[k] == lab.cls) en.named = 1;
-    if (e != 0.f) s[SUM_QD] += e * (t - (en.z[k] - m) * invt);
+    if (e != 0.f) s[SUM_QD] += e * (t - (en.z[k] - m));
   }
 }
 
@@ -156,7 +158,7 @@ __device__ inline float row_loss_of(const DistillArgs& a, float w, const float* 
   const bool some = s[SUM_T] != 0.f;
   float v = 0.f;
   if (some && s[SUM_Q] != 0.f)
-    v = a.alpha * a.temperature * a.temperature * (s[SUM_QD] / s[SUM_Q] + logf(s[SUM_T] / s[SUM_Q]));
+    v = a.alpha * a.temperature * (s[SUM_QD] / s[SUM_Q] + a.temperature * logf(s[SUM_T] / s[SUM_Q]));
   if (HARD && some && labelled) v += (1.0f - a.alpha) * (logf(s[SUM_1]) - (zlab - m));
   return w * v;
 }

@@ -1,8 +1,10 @@
 """The row operators at the limits of their arguments."""
+import numpy as np
 import pytest
 
+from oracle import rows
 from paper_2509_26092_amd import binding as B
-from test_gpu_rows import TOL, ws_of
+from test_gpu_rows import TOL, f64, mat, out, run_distill, ws_of
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +31,48 @@ def test_layernorm_bwd_of_the_widest_rows(prec, D):
     xh *= (g * xh).sum(dim=1, keepdim=True) / D
     want = rs.double()[:, None] * (g - g.sum(dim=1, keepdim=True) / D - xh)
     assert bool(((dx.double() - want).abs() <= (2.0 ** -8 if prec == "bf16" else 0.0) * want.abs() + TOL * 7).all())
+
+LOW = -3.4028234663852886e38
+
+
+# (rows, classes): sixteen lanes, a wave or a block a row, whole blocks of up
+# to 1024 lanes, and rows in parts
+@pytest.mark.parametrize("R,C", [(2100, 100), (1100, 1000), (8, 10), (8, 1000), (8, 33000), (70, 50001), (8, 200000)])
+@pytest.mark.parametrize("T", [0.5, 2.0 ** -50, 2.0 ** 70])
+def test_distill_teacher_values_of_the_whole_range(R, C, T):
+    """Teacher's values whose quotient by the temperature passes fp32's range:
+    a row of the lowest value throughout (equal shares), the lowest and the
+    highest beside others. Logits are small multiples of T where T is tiny
+    and of 1 elsewhere, so every loss and gradient is an ordinary number up to
+    the factors T^2 and T, which `scale` takes back for the gradient. Soft
+    terms of T = 2^70 are log(C / K) T^2, beyond fp32: infinite."""
+    rng = np.random.default_rng(R + C)
+    K = 4
+    z = rng.integers(-3, 4, (R, C)).astype(np.float64) * min(T, 1.0)
+    t_idx = np.stack([rng.permutation(C)[:K] for _ in range(R)]).astype(np.int32)
+    t_vals = rng.integers(-3, 4, (R, K)).astype(np.float32) * np.float32(min(T, 1.0))
+    t_vals[0] = LOW
+    t_vals[1] = [LOW, 1.0, 1.0, LOW]
+    t_vals[2] = [-LOW, -LOW, 1.0, 0.0]
+    t_vals[3] = [2.0 ** 100, 2.0 ** 100, 0.0, LOW]
+    t_vals[4, 0] = -np.inf
+    scale = 1.0 / T
+    zd, _ = mat(z, "fp32")
+    dzd, _ = out(R, C, "fp32")
+    row, _ = run_distill(zd, "fp32", t_vals, t_idx, None, None, K, T, 1.0, scale, R, C, C, dzd, C)
+    row_o, _, dz_o = rows.distill(zd.cpu().numpy(), t_vals, t_idx, None, None, T, 1.0, scale)
+    assert np.isfinite(f64(dzd)).all() and np.abs(f64(dzd) - dz_o).max() <= TOL * np.abs(dz_o).max()
+    if T > 1e19:
+        assert (row == np.inf).all() and (row_o > 3.5e38).all()
+    else:
+        assert np.abs(row / T ** 2 - row_o / T ** 2).max() <= TOL * np.abs(row_o / T ** 2).max()
+
+
+def test_distill_of_one_class_at_a_high_temperature():
+    """One class: nothing to learn, a loss of 0 at every temperature."""
+    zd, _ = mat(np.array([[3.0], [-2.0]]), "fp32")
+    dzd, _ = out(2, 1, "fp32")
+    for T in (1.0, 1e15, 1e25, 1e38):
+        row, loss = run_distill(zd, "fp32", np.ones((2, 1), np.float32), np.zeros((2, 1), np.int32), None, None, 1, T,
+                                1.0, 1.0 / T, 2, 1, 1, dzd, 1)
+        assert not row.any() and loss == 0.0 and not f64(dzd).any()
