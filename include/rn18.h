@@ -140,7 +140,7 @@ int rn18_train_step(rn18_ctx* ctx, float* state, const float* images, const int3
  *   labels  [N] int32, -1 for a sample without one (no label term; other
  *           labels outside [0, C) set RN18_ELABEL too); may be NULL for
  *           alpha = 1
- *   temperature > 0, alpha in [0, 1]
+ *   temperature (from 4.24e-39 on, finite) and alpha in [0, 1] as there
  * Dropout, loss scaling, errors and the update are those of
  * rn18_train_step. */
 int rn18_train_step_distill(rn18_ctx* ctx, float* state, const float* images, const int32_t* labels,

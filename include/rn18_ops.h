@@ -140,8 +140,9 @@ int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64
  * -inf and get a zero gradient. w: row_weight fp32 [R] (NULL: 1); a row of
  * weight 0 has loss 0 and gradient 0 whatever its logits hold.
  * row_loss fp32 [R]; loss 1 fp32 (may be NULL); dz as z (NULL: no gradient;
- * may be z itself). temperature > 0, alpha in [0, 1], scale finite (1/R for
- * the batch's mean, times a loss scale in fp16). */
+ * may be z itself). temperature positive and finite, from 4.24e-39 on (log2(e)
+ * over it is finite), alpha in [0, 1], scale finite (1/R for the batch's mean,
+ * times a loss scale in fp16). */
 size_t rn18op_distill_loss_workspace(int prec, int64_t R, int C, int K);
 int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int32_t* t_idx, const int32_t* labels,
                         const float* row_weight, void* dz, float* row_loss, float* loss, int64_t R, int C,

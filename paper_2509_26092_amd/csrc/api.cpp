@@ -1314,8 +1314,8 @@ int rn18_set_workspace(rn18_ctx* h, void* dev, size_t bytes) {
 
 // The checks of a loss's temperature and mix.
 static int mix_check(float temperature, float alpha) {
-  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.0f / temperature))
-    return fail(RN18_EINVAL, "the temperature must be positive and finite");
+  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(kLog2e / temperature))
+    return fail(RN18_EINVAL, "the temperature must be positive and finite, and log2(e) over it finite");
   if (!(alpha >= 0.f && alpha <= 1.f)) return fail(RN18_EINVAL, "alpha must be in [0, 1]");
   return RN18_OK;
 }

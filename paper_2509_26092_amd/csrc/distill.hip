@@ -32,7 +32,6 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
-constexpr float kLog2e = 1.44269504088896340736f;
 // 2^x by the hardware's instruction (1 ulp; 0 below 2^-126)
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -290,6 +290,7 @@ int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int 
 
 // Distillation against a teacher's top logits. labels, weight and dz may be
 // NULL; loss (optional) is written with scale * sum of the row losses.
+constexpr float kLog2e = 1.44269504088896340736f;   // exponentials are powers of 2 with the factor kLog2e / T
 struct DistillArgs {
   const void* z;
   const float* t_vals;
