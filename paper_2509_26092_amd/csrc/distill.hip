@@ -57,7 +57,8 @@ struct First {
 template <bool HARD>
 __device__ inline First load_first(const DistillArgs& a, long r, int l) {
   First f = {-1, -1, -INFINITY};
-  if (HARD) f.label = a.labels[r];
+  // (a step checks the labels whether or not its loss has a term for them)
+  if (HARD || (a.err && a.labels)) f.label = a.labels[r];
   if (l < a.K) {
     f.i = a.t_idx[r * a.K + l];
     f.t = a.t_vals[r * a.K + l];
@@ -76,10 +77,9 @@ struct Label {
 // gathered before, or NULL.
 template <typename T, bool HARD>
 __device__ inline Label load_label(const DistillArgs& a, int l, const First& f, const T* zr, const float* zk) {
-  if (!HARD) return {-1, 0.f};
   const int i = f.label;
-  if (i >= 0 && i < a.C) return {i, zk ? zk[a.K] : TT<T>::to_f(zr[i])};
-  if (a.err && i != -1 && l == 0) atomicOr(a.err, (unsigned)DEVERR_LABEL);
+  if (HARD && i >= 0 && i < a.C) return {i, zk ? zk[a.K] : TT<T>::to_f(zr[i])};
+  if (a.err && (i < -1 || i >= a.C) && l == 0) atomicOr(a.err, (unsigned)DEVERR_LABEL);
   return {-1, 0.f};
 }
 

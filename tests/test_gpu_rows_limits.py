@@ -76,3 +76,26 @@ def test_distill_of_one_class_at_a_high_temperature():
         row, loss = run_distill(zd, "fp32", np.ones((2, 1), np.float32), np.zeros((2, 1), np.int32), None, None, 1, T,
                                 1.0, 1.0 / T, 2, 1, 1, dzd, 1)
         assert not row.any() and loss == 0.0 and not f64(dzd).any()
+
+
+@pytest.mark.parametrize("classes", [10, 70000])
+def test_step_flags_bad_labels_that_no_term_reads(classes):
+    """alpha = 1: the labels have no part in the loss, and one that is
+    neither a class nor -1 is still reported."""
+    import torch
+    N = 4
+    w = B.Worker("tiny", classes, "fp32")
+    state = torch.zeros(w.n_state, device="cuda")
+    B.rn18_destroy(B.rn18_init(w.cfg, 3, state))
+    x = torch.randn((N, 3, 16, 16), device="cuda")
+    vals = torch.randn((N, 3), device="cuda")
+    idx = torch.arange(3 * N, device="cuda", dtype=torch.int32).view(N, 3) % classes
+    for bad, want in ((0, B.RN18_OK), (-1, B.RN18_OK), (classes, B.RN18_ELABEL), (-2, B.RN18_ELABEL)):
+        y = torch.zeros(N, device="cuda", dtype=torch.int32)
+        y[N - 1] = bad
+        for alpha in (1.0, 0.5):
+            w.train_step_distill(state, x, y, vals, idx, 2.0, alpha, 0.0)
+            assert w.sync_status() == want, (bad, alpha)
+    w.train_step_distill(state, x, None, vals, idx, 2.0, 1.0, 0.0)
+    assert w.sync_status() == B.RN18_OK
+    w.close()
