@@ -181,7 +181,7 @@ struct Plan {
   size_t x0, zstem, pool, parg;
   int Hs, Ws, Hp, Wp;           // stem output and pool output sizes
   int Hf, Wf;                   // final feature map
-  size_t f, logits, dlogits, df, rowloss, lossbuf, distill;
+  size_t f, logits, dlogits, df, rowloss, lossbuf;
   // gy[p], gy2[p]: dY of the second and first conv of the blocks of index
   // parity p (gy[1] also takes the stem's dY); gyd: dY of a projection
   size_t gA, gB, gz, gy[2], gy2[2], gyd;
@@ -449,10 +449,10 @@ int build_plan(const Ctx& c, int N, int H, int W, Plan* pl, std::string* why) {
   pl->df = alloc((size_t)N * a.feat * 4);
   pl->rowloss = alloc((size_t)N * 4);
   pl->lossbuf = alloc(4);
-  // (of a step with a teacher; only few rows of tens of thousands of classes need any)
-  const size_t dws = distill_workspace(RN18_FP32, N, C, kTopMax);
-  pl->distill = dws ? alloc(dws) : 0;
-  pl->gA = alloc(max_blockio);
+  // The parts of a step's distillation loss (few rows of tens of thousands of
+  // classes have any) are in gA: the loss comes before the first gradient of an
+  // activation. They fit but for images of a few pixels.
+  pl->gA = alloc(std::max(max_blockio, distill_workspace(RN18_FP32, N, C, kTopMax)));
   pl->gB = alloc(max_blockio);
   pl->gz = alloc(max_z1 ? max_z1 : 16);
   pl->gy[0] = alloc(max_yb ? max_yb : 16);
@@ -862,7 +862,7 @@ int run_train(Ctx* c, const Plan& pl, float* state, const float* images, const i
     t.err = c->err;
     t.ls = c->ls;
     TIMED(RN18_K_HEAD, 7, 0, "distill_row_kernel", 0.0, 8.0 * N * (C + t.K),
-          distill_launch(RN18_FP32, t, lossp, ws + pl.distill, st));
+          distill_launch(RN18_FP32, t, lossp, ws + pl.gA, st));
   } else {
     TIMED(RN18_K_HEAD, 1, 0, "softmax_ce_kernel", 0.0, 8.0 * N * C,
           softmax_ce_launch(logits, labels, N, C, dlog, (float*)(ws + pl.rowloss), lossp, c->err, st, c->ls));

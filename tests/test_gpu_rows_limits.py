@@ -99,3 +99,16 @@ def test_step_flags_bad_labels_that_no_term_reads(classes):
     w.train_step_distill(state, x, None, vals, idx, 2.0, 1.0, 0.0)
     assert w.sync_status() == B.RN18_OK
     w.close()
+
+
+def test_workspace_of_a_step_does_not_grow_by_rows_in_parts():
+    """Rows of more than 65,536 fp32 classes are joined from parts in a step
+    with a teacher. Their room is memory that the backward pass needs anyway:
+    the workspace grows by the same amount a class below and above. (Sizes
+    where no other buffer changes its kind.)"""
+    ctx = {c: B.Worker("tiny", c, "fp32") for c in range(65408, 65665, 64)}
+    n = {c: B.rn18_workspace_bytes(w.ctx, 100, 16, 16) for c, w in ctx.items()}
+    step = n[65472] - n[65408]
+    assert step > 0
+    for c in (65472, 65536, 65600):
+        assert n[c + 64] - n[c] == step, c
