@@ -18,15 +18,23 @@ EPS = 1e-5
 
 
 def teacher_targets(worker, state, images, k):
-    """(values, classes) [N][k] of the teacher's largest logits for a batch."""
+    """(values, classes) [N][k] of the teacher's largest logits for a batch.
+    All of it runs on the worker's stream, after what is on the current one
+    (the images, the state); the current stream waits for the result."""
     n, c = images.shape[0], worker.cfg.num_classes
-    logits = torch.empty((n, c), device="cuda")
-    worker.eval_logits(state, images, logits)
-    vals = torch.empty((n, k), device="cuda")
-    idx = torch.empty((n, k), dtype=torch.int32, device="cuda")
-    need = B.rn18op_topk_logits_workspace(B.RN18_FP32, n, c, k)
-    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
-    B.rn18op_topk_logits(B.RN18_FP32, logits, vals, idx, n, c, logits.stride(0), k, ws)
+    here = torch.cuda.current_stream()
+    worker.stream.wait_stream(here)
+    with torch.cuda.stream(worker.stream):
+        logits = torch.empty((n, c), device="cuda")
+        worker.eval_logits(state, images, logits)
+        vals = torch.empty((n, k), device="cuda")
+        idx = torch.empty((n, k), dtype=torch.int32, device="cuda")
+        need = B.rn18op_topk_logits_workspace(B.RN18_FP32, n, c, k)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+        B.rn18op_topk_logits(B.RN18_FP32, logits, vals, idx, n, c, logits.stride(0), k, ws)
+    here.wait_stream(worker.stream)
+    for t in (vals, idx):           # made on the worker's stream, read on the current one
+        t.record_stream(here)
     return vals, idx
 
 
