@@ -130,14 +130,23 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_current_handle = None   # the function that gives the handle of torch's current stream
+
+
 def _stream(stream=None):
-    """The HIP stream of `stream`, or torch's current one. Its handle is asked
-    for directly: building a torch.cuda.Stream object takes 2.8 us, as long
-    as a kernel launch (8.0 -> 4.9 us for a whole call of a small operator)."""
+    """The HIP stream of `stream`, or torch's current one. torch is asked for
+    its handle by device where it can be: 0.3 us in place of the 2.8 of a
+    torch.cuda.Stream object (a layer norm of 64x512 fp32, one call after the
+    other: 5.2 and 7.7 us)."""
+    global _current_handle
     if stream is not None:
         return stream.cuda_stream
-    import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if _current_handle is None:
+        import torch
+        by_device, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        _current_handle = (lambda: by_device(device())) if by_device else \
+            (lambda: torch.cuda.current_stream().cuda_stream)
+    return _current_handle()
 
 
 def make_config(arch, num_classes, prec="fp32", momentum=0.9, weight_decay=5e-4, bn_eps=1e-5, bn_momentum=0.1):
