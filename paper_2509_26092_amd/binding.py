@@ -5,6 +5,11 @@ Argument marshalling only: torch tensors provide device memory
 (``data_ptr()``) and the HIP stream (``torch.cuda.current_stream()``); every
 step of the computation runs in the library's HIP kernels. If the library is
 not built, importing a function raises instead of falling back to anything.
+
+Sizes and strides are the caller's. What a caller takes from torch in another
+type than the library's (classes of torch.topk in int64, values and scales in
+16 bits) is refused by the row operators, and a Worker refuses a teacher's
+list or labels of other sizes than the batch's.
 """
 import ctypes
 import os
@@ -130,20 +135,46 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+class _Types(dict):
+    """torch's type of a name, looked up once."""
+
+    def __missing__(self, name):
+        import torch
+        t = self[name] = getattr(torch, name)
+        return t
+
+
+_types = _Types()
+
+
+def _arr(t, kind, name, n=0):
+    """The pointer of an array of type `kind` with n elements at least, or
+    None. (0.1 us more than _ptr, with n 0.3.)"""
+    if t is None:
+        return None
+    if t.dtype is _types[kind] and (not n or t.numel() >= n and t.is_contiguous()):
+        return t.data_ptr()
+    raise Rn18Error(RN18_EINVAL, "%s must be %s%s, not %s of shape %s and strides %s"
+                    % (name, kind, ", %d elements one after the other" % n if n else "", t.dtype, tuple(t.shape),
+                       t.stride()))
+
+
 _current_handle = None   # the function that gives the handle of torch's current stream
 
 
 def _stream(stream=None):
     """The HIP stream of `stream`, or torch's current one. torch is asked for
-    its handle by device where it can be: 0.3 us in place of the 2.8 of a
+    its handle by device where it can be: 0.2 us in place of the 2.9 of a
     torch.cuda.Stream object (a layer norm of 64x512 fp32, one call after the
-    other: 5.2 and 7.7 us)."""
+    other: 4.7 and 7.6 us)."""
     global _current_handle
     if stream is not None:
         return stream.cuda_stream
     if _current_handle is None:
         import torch
-        by_device, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        by_device = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        torch.cuda.current_device()   # (starts CUDA, which its own short form expects)
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _current_handle = (lambda: by_device(device())) if by_device else \
             (lambda: torch.cuda.current_stream().cuda_stream)
     return _current_handle()
@@ -183,8 +214,10 @@ def rn18_train_step(ctx, state, images, labels, N, H, W, lr, loss=None):
 
 
 def rn18_train_step_distill(ctx, state, images, labels, t_vals, t_idx, K, temperature, alpha, N, H, W, lr, loss=None):
-    return _check(lib().rn18_train_step_distill(ctx, _ptr(state), _ptr(images), _ptr(labels), _ptr(t_vals),
-                                                _ptr(t_idx), K, temperature, alpha, N, H, W, lr, _ptr(loss)))
+    return _check(lib().rn18_train_step_distill(ctx, _ptr(state), _ptr(images), _arr(labels, "int32", "labels", N),
+                                                _arr(t_vals, "float32", "t_vals", N * K),
+                                                _arr(t_idx, "int32", "t_idx", N * K), K, temperature, alpha, N, H, W,
+                                                lr, _ptr(loss)))
 
 
 def rn18_eval_logits(ctx, state, images, N, H, W, logits):
@@ -293,8 +326,10 @@ def _ws(t):
 
 
 def rn18op_layernorm_fwd(prec, x, gamma, beta, y, mean, rstd, R, D, ldx, ldy, eps=1e-5, stream=None):
-    return _check(lib().rn18op_layernorm_fwd(prec, _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
-                                             R, D, ldx, ldy, eps, _stream(stream)))
+    r = (_lib or lib()).rn18op_layernorm_fwd(prec, _ptr(x), _arr(gamma, "float32", "gamma"),
+                                             _arr(beta, "float32", "beta"), _ptr(y), _ptr(mean), _ptr(rstd), R, D, ldx,
+                                             ldy, eps, _stream(stream))
+    return _check(r) if r else r
 
 
 def rn18op_layernorm_bwd_workspace(prec, R, D):
@@ -303,9 +338,11 @@ def rn18op_layernorm_bwd_workspace(prec, R, D):
 
 def rn18op_layernorm_bwd(prec, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, R, D, lddy, ldx, lddx, ws=None,
                          stream=None):
-    return _check(lib().rn18op_layernorm_bwd(prec, _ptr(dy), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dx),
-                                             _ptr(dgamma), _ptr(dbeta), R, D, lddy, ldx, lddx, *_ws(ws),
-                                             _stream(stream)))
+    r = (_lib or lib()).rn18op_layernorm_bwd(prec, _ptr(dy), _ptr(x), _arr(gamma, "float32", "gamma"), _ptr(mean),
+                                             _ptr(rstd), _ptr(dx), _arr(dgamma, "float32", "dgamma"),
+                                             _arr(dbeta, "float32", "dbeta"), R, D, lddy, ldx, lddx, *_ws(ws),
+                                             _stream(stream))
+    return _check(r) if r else r
 
 
 def rn18op_topk_logits_workspace(prec, R, C, K):
@@ -313,8 +350,9 @@ def rn18op_topk_logits_workspace(prec, R, C, K):
 
 
 def rn18op_topk_logits(prec, z, vals, idx, R, C, ldz, K, ws=None, stream=None):
-    return _check(lib().rn18op_topk_logits(prec, _ptr(z), _ptr(vals), _ptr(idx), R, C, ldz, K, *_ws(ws),
-                                           _stream(stream)))
+    r = (_lib or lib()).rn18op_topk_logits(prec, _ptr(z), _arr(vals, "float32", "vals"), _arr(idx, "int32", "idx"), R,
+                                           C, ldz, K, *_ws(ws), _stream(stream))
+    return _check(r) if r else r
 
 
 def rn18op_distill_loss_workspace(prec, R, C, K):
@@ -323,9 +361,13 @@ def rn18op_distill_loss_workspace(prec, R, C, K):
 
 def rn18op_distill_loss(prec, z, t_vals, t_idx, labels, row_weight, dz, row_loss, loss, R, C, ldz, lddz, K,
                         temperature, alpha, scale, ws=None, stream=None):
-    return _check(lib().rn18op_distill_loss(prec, _ptr(z), _ptr(t_vals), _ptr(t_idx), _ptr(labels), _ptr(row_weight),
-                                            _ptr(dz), _ptr(row_loss), _ptr(loss), R, C, ldz, lddz, K, temperature,
-                                            alpha, scale, *_ws(ws), _stream(stream)))
+    n = R * K
+    r = (_lib or lib()).rn18op_distill_loss(prec, _ptr(z), _arr(t_vals, "float32", "t_vals", n),
+                                            _arr(t_idx, "int32", "t_idx", n), _arr(labels, "int32", "labels", R),
+                                            _arr(row_weight, "float32", "row_weight", R), _ptr(dz), _ptr(row_loss),
+                                            _ptr(loss), R, C, ldz, lddz, K, temperature, alpha, scale, *_ws(ws),
+                                            _stream(stream))
+    return _check(r) if r else r
 
 
 DBG = dict(y=0, z1=1, out=2, gA=3, gB=4, gz=5, gy=6, gyd=7, grad=8, wf=9, wd=10, mean=11, rstd=12, zstem=13,
@@ -391,11 +433,22 @@ class Worker:
         return rn18_train_step(self.ctx, state, images, labels, N, H, W, lr, loss)
 
     def train_step_distill(self, state, images, labels, t_vals, t_idx, temperature, alpha, lr, loss=None):
-        """A step against a teacher's top logits t_vals, t_idx [N][K]."""
+        """A step against a teacher's top logits: t_vals fp32 and t_idx int32
+        [N][K], labels int32 [N] or None for alpha = 1, all contiguous and on
+        the images' device."""
         N, _, H, W = images.shape
+        K = t_vals.shape[-1]
+        for t, kind, shape, name in ((t_vals, "float32", (N, K), "t_vals"), (t_idx, "int32", (N, K), "t_idx"),
+                                     (labels, "int32", (N,), "labels")):
+            if t is None:
+                continue
+            if tuple(t.shape) != shape or t.device != images.device:
+                raise Rn18Error(RN18_EINVAL, "%s must be of shape %s on %s, not %s on %s"
+                                % (name, shape, images.device, tuple(t.shape), t.device))
+            _arr(t, kind, name, t.numel())
         self._ensure(N, H, W)
-        return rn18_train_step_distill(self.ctx, state, images, labels, t_vals, t_idx, t_vals.shape[1], temperature,
-                                       alpha, N, H, W, lr, loss)
+        return rn18_train_step_distill(self.ctx, state, images, labels, t_vals, t_idx, K, temperature, alpha, N, H, W,
+                                       lr, loss)
 
     def eval_logits(self, state, images, logits):
         N, _, H, W = images.shape
