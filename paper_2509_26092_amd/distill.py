@@ -38,6 +38,15 @@ def teacher_targets(worker, state, images, k):
     return vals, idx
 
 
+def _rows(t):
+    """`t` [rows][width] and its row stride: as it is where the elements of a
+    row are one after the other and rows do not overlap, otherwise a copy."""
+    r, d = t.shape
+    if (d > 1 and t.stride(1) != 1) or (r > 1 and t.stride(0) < d):
+        t = t.contiguous()
+    return t, t.stride(0) if r > 1 else d
+
+
 class LayerNorm:
     """Layer norm over the last axis of [rows][width]: parameters, what the
     backward pass needs, and gradients."""
@@ -49,21 +58,28 @@ class LayerNorm:
 
     def forward(self, x):
         r, d = x.shape
+        if d != len(self.gamma):
+            raise ValueError("rows of %d elements for a layer norm of %d" % (d, len(self.gamma)))
         self.prec = {torch.float32: B.RN18_FP32, torch.bfloat16: B.RN18_BF16, torch.float16: B.RN18_FP16}[x.dtype]
-        self.x, y = x, torch.empty_like(x)
+        self.x, self.ldx = _rows(x)
+        y = torch.empty((r, d), dtype=x.dtype, device=x.device)
         self.mean, self.rstd = torch.empty(r, device="cuda"), torch.empty(r, device="cuda")
-        B.rn18op_layernorm_fwd(self.prec, x, self.gamma, self.beta, y, self.mean, self.rstd, r, d, x.stride(0),
-                               y.stride(0), EPS)
+        B.rn18op_layernorm_fwd(self.prec, self.x, self.gamma, self.beta, y, self.mean, self.rstd, r, d, self.ldx, d,
+                               EPS)
         return y
 
     def backward(self, dy):
-        """The gradient of the forward pass's input, in place of dy."""
+        """The gradient of the forward pass's input, in place of dy unless its
+        rows have to be copied."""
         r, d = dy.shape
+        if dy.shape != self.x.shape or dy.dtype != self.x.dtype:
+            raise ValueError("a gradient of another shape or type than the forward pass's input")
+        dy, ld = _rows(dy)
         need = B.rn18op_layernorm_bwd_workspace(self.prec, r, d)
         if self.ws is None or self.ws.numel() < need:
             self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
         B.rn18op_layernorm_bwd(self.prec, dy, self.x, self.gamma, self.mean, self.rstd, dy, self.dgamma, self.dbeta, r,
-                               d, dy.stride(0), self.x.stride(0), dy.stride(0), self.ws)
+                               d, ld, self.ldx, ld, self.ws)
         return dy
 
 
