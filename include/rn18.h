@@ -32,10 +32,11 @@
  *    step takes up to 21,232 images, more than 288 GB of memory hold; see
  *    rn18_workspace_bytes), or a non-finite factor. rn18_last_error()
  *    returns a thread-local description of the last non-OK return.
- *  - Errors found on the device (a bad label, a non-finite image
- *    value or a non-finite loss) set a sticky flag of the context; the call
- *    still runs to completion, and rn18_sync_status reports and clears the
- *    flag.
+ *  - Errors found on the device (a label or a class of a teacher's list
+ *    outside [0, C), where a step with a teacher takes -1 for none, a
+ *    non-finite image value or a non-finite loss) set a sticky flag of the
+ *    context; the call still runs to completion, and rn18_sync_status reports
+ *    and clears the flag.
  *  - No C++ exception crosses this interface.
  */
 #ifndef RN18_H
@@ -138,8 +139,8 @@ int rn18_train_step(rn18_ctx* ctx, float* state, const float* images, const int3
  *           fills a short list, other classes outside [0, C) are left out and
  *           set RN18_ELABEL
  *   labels  [N] int32, -1 for a sample without one (no label term; other
- *           labels outside [0, C) set RN18_ELABEL too); may be NULL for
- *           alpha = 1
+ *           labels outside [0, C) set RN18_ELABEL too, whatever alpha is);
+ *           may be NULL for alpha = 1
  *   temperature (from 4.24e-39 on, finite) and alpha in [0, 1] as there
  * Dropout, loss scaling, errors and the update are those of
  * rn18_train_step. */

@@ -1451,7 +1451,7 @@ int rn18_sync_status(rn18_ctx* h) {
     LCHK(fill_zero_launch(c.err, 4, c.stream));
     HIPCHK(hipStreamSynchronize(c.stream));
   }
-  if (e & DEVERR_LABEL) return fail(RN18_ELABEL, "a label was outside [0, num_classes)");
+  if (e & DEVERR_LABEL) return fail(RN18_ELABEL, "a label, or a class of a teacher's list, was outside [0, num_classes)");
   if (e & DEVERR_NONFINITE) return fail(RN18_ENONFINITE, "the loss was not finite");
   return RN18_OK;
 }

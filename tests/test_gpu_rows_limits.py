@@ -112,3 +112,18 @@ def test_workspace_of_a_step_does_not_grow_by_rows_in_parts():
     assert step > 0
     for c in (65472, 65536, 65600):
         assert n[c + 64] - n[c] == step, c
+
+
+def test_status_names_the_teachers_list():
+    """A class of the teacher's list outside [0, C) sets the same status as
+    such a label: its text names both."""
+    import torch
+    w = B.Worker("tiny", 10, "fp32")
+    state = torch.zeros(w.n_state, device="cuda")
+    B.rn18_destroy(B.rn18_init(w.cfg, 3, state))
+    idx = torch.tensor([[1, 10], [2, 3]], device="cuda", dtype=torch.int32)
+    w.train_step_distill(state, torch.randn((2, 3, 16, 16), device="cuda"), None, torch.randn((2, 2), device="cuda"),
+                         idx, 2.0, 1.0, 0.0)
+    assert w.sync_status() == B.RN18_ELABEL
+    assert "label" in B.rn18_last_error() and "teacher" in B.rn18_last_error()
+    w.close()
