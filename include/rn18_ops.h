@@ -97,7 +97,8 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* hip_stream);
  *   y = (x - mean) * rstd * gamma + beta
  * gamma, beta fp32 [D] (NULL: 1 and 0); mean, rstd fp32 [R], kept for the
  * backward pass (NULL in inference). A row that holds a NaN or an infinity
- * gives NaN. */
+ * gives NaN. The sums are fp32's: where the squares of x - mean pass its range
+ * (from 1.8e19 on) rstd is 0, and where a row's sum does the row is NaN. */
 int rn18op_layernorm_fwd(int prec, const void* x, const float* gamma, const float* beta, void* y, float* mean,
                          float* rstd, int64_t R, int D, int64_t ldx, int64_t ldy, float eps, void* hip_stream);
 
@@ -133,11 +134,14 @@ int rn18op_topk_logits(int prec, const void* z, float* vals, int32_t* idx, int64
  * any order; an entry that is not valid is left out (a short list is filled
  * with t_idx = -1), and entries of one class add up. Terms with q_k = 0 are 0.
  * alpha = 0 leaves out the soft term and alpha = 1 the hard one, whatever
- * their inputs hold; otherwise a teacher's NaN or +inf makes its row NaN. A
- * listed class that the student masks has an infinite loss. A row without a valid entry has no soft term; one whose label is outside
- * [0, C) (-1, say; labels NULL: every row) has no hard term; a row whose
- * logits are all -inf (every class masked) has neither. Masked classes hold
- * -inf and get a zero gradient. w: row_weight fp32 [R] (NULL: 1); a row of
+ * their inputs hold; otherwise a valid entry of NaN or +inf makes its row's
+ * loss and the gradient of the row's listed classes NaN (the other classes'
+ * gradient needs the student's logits alone and stays a number). A listed
+ * class that the student masks has an infinite loss, and a loss beyond fp32
+ * is infinite. A row without a valid entry has no soft term; one whose label
+ * is outside [0, C) (-1, say; labels NULL: every row) has no hard term; a row
+ * whose logits are all -inf (every class masked) has neither. Masked classes
+ * hold -inf and get a zero gradient. w: row_weight fp32 [R] (NULL: 1); a row of
  * weight 0 has loss 0 and gradient 0 whatever its logits hold.
  * row_loss fp32 [R]; loss 1 fp32 (may be NULL); dz as z (NULL: no gradient;
  * may be z itself). temperature positive and finite, from 4.24e-39 on (log2(e)

@@ -4,7 +4,7 @@ import pytest
 
 from oracle import rows
 from paper_2509_26092_amd import binding as B
-from test_gpu_rows import TOL, f64, mat, out, run_distill, ws_of
+from test_gpu_rows import TOL, distill_inputs, f64, mat, out, run_distill, ws_of
 
 pytestmark = pytest.mark.gpu
 
@@ -127,3 +127,44 @@ def test_status_names_the_teachers_list():
     assert w.sync_status() == B.RN18_ELABEL
     assert "label" in B.rn18_last_error() and "teacher" in B.rn18_last_error()
     w.close()
+
+
+@pytest.mark.parametrize("R,C", [(2100, 100), (8, 10), (8, 1000), (8, 33000), (70, 50001), (8, 200000)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_distill_teacher_without_a_number(R, C, bad):
+    """A teacher's NaN or +inf: its row's loss and the gradient of the classes
+    that the row lists are NaN; the other classes' gradient, which needs the
+    student's logits alone, and every other row are as without it."""
+    K = 5
+    z, t_vals, t_idx, labels, _ = distill_inputs("fp32", R, C, K, False, seed=4)
+    t_vals[1, 2] = bad
+    zd, _ = mat(z, "fp32")
+    dzd, _ = out(R, C, "fp32")
+    row, loss = run_distill(zd, "fp32", t_vals, t_idx, labels, None, K, 2.0, 0.5, 1.0, R, C, C, dzd, C)
+    with np.errstate(all="ignore"):
+        row_o, _, dz_o = rows.distill(z, t_vals, t_idx, labels, None, 2.0, 0.5, 1.0)
+    dz = f64(dzd)
+    listed = np.zeros((R, C), bool)
+    listed[1, t_idx[1]] = True
+    assert np.array_equal(np.isnan(dz), listed) and np.array_equal(np.isnan(dz_o), listed)
+    assert np.abs(dz - dz_o)[~listed].max() <= TOL * np.abs(dz_o[~listed]).max()
+    good = np.arange(R) != 1
+    assert np.isnan(row[1]) and np.isnan(loss) and np.allclose(row[good], row_o[good], rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("D", [3, 64, 1001, 8192, 33000])
+def test_layernorm_beyond_the_sums_range(D):
+    """Squares beyond fp32's range: rstd 0 and rows of beta. Sums beyond it:
+    NaN. The rows beside them are as ever."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.randn((4, D), device="cuda", generator=g)
+    x[1, 0], x[1, 1] = 1e20, -1e20
+    x[2, :2] = 3e38
+    beta = torch.randn(D, device="cuda", generator=g)
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
+    B.rn18op_layernorm_fwd(B.RN18_FP32, x, None, beta, y, mean, rstd, 4, D, D, D)
+    assert rstd[1].item() == 0.0 and torch.equal(y[1], beta)
+    assert bool(y[2].isnan().all())
+    want, _, _ = rows.layernorm_forward(x[0::3].cpu().double().numpy(), None, beta.cpu().double().numpy(), 1e-5)
+    assert np.abs(f64(y[0::3]) - want).max() <= TOL * np.abs(want).max()
