@@ -184,3 +184,31 @@ def test_distill_lanes_and_chunks(prec, R, C, K, T, alpha, masked, pad, off):
     row2, _ = run_distill(zd, prec, t_vals, t_idx, labels, weight, K, T, alpha, scale, R, C, C + pad, zd, C + pad,
                           want_loss=False)
     assert torch.equal(dzd, zd) and np.array_equal(row, row2)      # in place of z, bit for bit
+
+
+# ---------------------------------------------------------------- every kernel
+# 16-byte chunks of a row: one width for each number of lanes and of chunks a lane
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("chunks", [1, 2, 3, 7, 15, 31, 60, 120, 180, 250, 500, 700, 1000, 1400, 2000, 2900, 4000])
+def test_layernorm_every_width(prec, chunks):
+    """Few rows, and for rows within a wave as many as take two rows a lane
+    at once; whole chunks, and a tail beside them."""
+    vw = 4 if prec == "fp32" else 8
+    lanes = min(64, 1 << (chunks - 1).bit_length())
+    for R in [37] + ([256 * (256 // lanes) * 4 + 3] if chunks <= 64 else []):
+        for D in (chunks * vw, chunks * vw + 3):
+            test_layernorm_fwd_many_rows(prec, R, D, 0, 0, False)
+            test_layernorm_bwd_many_rows(prec, R, D, 0, 0, None)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("alpha", [1.0, 0.5])
+@pytest.mark.parametrize("R,chunks", [(2050, 15), (2050, 30), (2050, 60), (1030, 60), (1030, 120), (1030, 250),
+                                      (1030, 500), (300, 200), (300, 400), (300, 1000), (140, 2000), (66, 4000),
+                                      (66, 8000), (66, 16000)])
+def test_distill_every_width(prec, alpha, R, chunks):
+    """Sixteen lanes, a wave and blocks of 256 to 1024 lanes, with the
+    labels' term and without (a list of 70 keeps 60 chunks in a wave)."""
+    vw = 4 if prec == "fp32" else 8
+    test_distill_lanes_and_chunks(prec, R, chunks * vw + 1, 70 if (R, chunks) == (1030, 60) else 9, 2.0, alpha, True, 1,
+                                  0)
