@@ -7,16 +7,16 @@
 //
 // z is read once into registers, its maximum and sums of exponentials are
 // taken there, and dz is written from there: 4 bytes of traffic and two or
-// four exponentials an element in 16 bits. Bound by memory without labels
-// (16384x32768 bf16, 64 listed, 449 us, 4.8 TB/s), with labels by memory and
-// the vector units together (4096x131071 bf16 585 us, without 475). The few
-// classes that the list or the label name are written a second time with
-// their own terms, by the lane of the first entry that names each. With
-// sum q = 1 the soft term is
+// four exponentials an element in 16 bits (four with labels, for alpha = 0
+// too). Bound by memory without labels (16384x32768 bf16, 64 listed, 441 us,
+// 4.9 TB/s), with labels by memory and the vector units together (4096x131071
+// bf16 583 us, without 472). The few classes that the list or the label name
+// are written a second time with their own terms, by the lane of the first
+// entry that names each. With sum q = 1 the soft term is
 // alpha T (sum_k q_k (t_k - z_k) + T (log sum e^z' - log sum e^t')), t and z
 // less their maxima, t' and z' over T too, so that every sum of a row is taken
-// in one step. The maxima are taken out before the division by T and the
-// sum over the entries is multiplied by T once: no quotient by a small T, nor T^2,
+// in one step. The maxima are taken out before the division by T and the sum
+// over the entries is multiplied by T once: no quotient by a small T, nor T^2,
 // leaves fp32's range on the way.
 #include <math.h>
 
@@ -32,7 +32,12 @@ namespace {
 
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
-// 2^x by the hardware's instruction (1 ulp; 0 below 2^-126)
+// 2^x by the hardware's instruction (1 ulp; 0 below 2^-126). e^-d is taken as
+// 2^(-d log2(e)) with the product rounded to 32 bits: an exponential is off by
+// up to about d 2^-24 of itself, and by d e^-d 2^-24, less than half a
+// rounding, of the row's largest, which the sums and the gradient are added to.
+// Against 64 bits the loss and gradient of 64x1000 fp32 rows are off by 0.9e-7,
+// those of library exponentials and a division by T by 1.2e-7.
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The teacher's list of a row; -1 fills its classes up to a multiple of 4.

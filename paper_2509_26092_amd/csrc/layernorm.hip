@@ -790,9 +790,10 @@ int layernorm_fwd_launch(int prec, const void* x, const float* gamma, const floa
 
 // Calls whose parameter gradients blocks of their own add up, in place of a
 // second launch that joins partial sums: dy and x are read twice, from cache,
-// and a column's sum is a chain of R / 32 additions. (A call on 64x512 fp32:
-// 6.1 us, with the second launch 9.7; 512x8192 bf16 13.0 and 20.4; but
-// 2048x1024 bf16 13.3 and 9.4.)
+// and a column's sum is a chain of R / 32 additions. (Calls one after the
+// other on the same inputs: 64x512 fp32 6.6 us, with the second launch 9.1 to
+// 10; 512x8192 bf16 13.6 and 23; 1024x4096 11.1 and 18; but 2048x1024 10.0 and
+// 9.5 to 10.6, 4096x512 16.9 and 10.1.)
 static bool ln_bwd_small(int prec, long R, int D) {
   return R <= 1024 && R * D * prec_bytes(prec) <= (8l << 20);
 }

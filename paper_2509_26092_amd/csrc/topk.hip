@@ -64,7 +64,7 @@ __device__ inline uint32_t kth_key(F key, int K) {   // key(p): the lane's p-th
     for (int p = 0; p < PER; ++p) n += __popcll(__ballot(key(p) >= c));
     return n >= K;
   };
-  // from 2 to 2^32, with the sign: where the K-th logit of most rows lies
+  // from 2 to 2^33, with the sign: where the K-th logit of most rows lies
   uint32_t t = 0xc0000000u;
   int b = 28;
   if (!enough(t) || enough(0xd0000000u)) {
@@ -406,10 +406,10 @@ struct TopPlan {
   int parts, len;
 };
 // Rows of more than 2^14 chunks, more than a block keeps the maxima of, are
-// cut into parts of up to 2^13 (512 rows of 131071 fp32 logits: 58 us; in
-// parts of 2^14, of which a compute unit holds one at a time, 69 us; fewer
-// rows or shorter ones gain nothing from parts: the launch that joins them
-// costs what they save).
+// cut into parts of up to 2^13 (512 rows of 131071 fp32 logits: 45 us, 2048
+// rows 191; in parts of 2^14, of which a compute unit holds one at a time, 58
+// and 225; fewer rows or shorter ones gain nothing from parts: the launch that
+// joins them costs what they save).
 TopPlan topk_plan(int prec, int C, int K) {
   const int vw = prec_vw(prec);
   if (C / vw <= 16384) return {1, C};
@@ -459,7 +459,10 @@ int topk_launch(int prec, const void* z, float* vals, int32_t* idx, long R, int 
       // Every logit's key takes part in the bound: rows to 256 logits (335544x100
       // bf16, 10 kept: 107 us, with maxima of chunks 176; 64 kept: 207 and 501),
       // longer ones whose chunks are too few for a bound (16384x512 bf16, 100
-      // kept: 62 and 445; 40 kept, from 64 chunks: 33 and 23).
+      // kept: 60 and 444, 52 kept: 37 and 54; 8192x1024, 256 kept: 136 and 874;
+      // but 40 kept of 512, from 64 chunks: 33 and 23). At the rule's edge the
+      // two cross within a tenth: 8192x1024, 100 kept: 66 and 63, 8388x1000 71
+      // and 64.
       const int chunks = C / TT<T>::VW;
       if (C <= 64) SHORT(1);
       if (C <= 128) SHORT(2);
