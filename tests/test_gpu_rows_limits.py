@@ -168,3 +168,64 @@ def test_layernorm_beyond_the_sums_range(D):
     assert bool(y[2].isnan().all())
     want, _, _ = rows.layernorm_forward(x[0::3].cpu().double().numpy(), None, beta.cpu().double().numpy(), 1e-5)
     assert np.abs(f64(y[0::3]) - want).max() <= TOL * np.abs(want).max()
+
+
+def test_rows_of_2_30_elements():
+    """The widest rows the operators take, one short of whole chunks by
+    three, in bf16: positions to the end of the range. A lane adds 2^20
+    terms in a chain here: their roundings come to about 1e-5 of the sum."""
+    import torch
+    D, U, tol = 2 ** 30 - 3, 2.0 ** -8, 1e-4
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((1, D), device="cuda", generator=g, dtype=torch.bfloat16)
+    x64 = x.double()
+    m = x64.mean()
+    x64 -= m
+    rs = 1.0 / torch.sqrt((x64 * x64).mean() + 1e-5)
+    x64 *= rs
+    y, mean, rstd = torch.empty_like(x), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    B.rn18op_layernorm_fwd(B.RN18_BF16, x, None, None, y, mean, rstd, 1, D, D, D)
+    assert abs(mean.item() - m.item()) <= tol and abs(rstd.item() / rs.item() - 1) <= tol
+    assert bool(((y.double() - x64).abs() <= U * x64.abs() + tol * 7).all())
+    # the gradient of dy = y: xh is y up to a rounding, and so is what remains of dy after its projections
+    dgamma, dbeta = torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    dx = torch.empty_like(x)
+    B.rn18op_layernorm_bwd(B.RN18_BF16, y, x, None, mean, rstd, dx, dgamma, dbeta, 1, D, D, D, D,
+                           ws_of(B.rn18op_layernorm_bwd_workspace(B.RN18_BF16, 1, D)))
+    assert torch.equal(dbeta, y[0].float())
+    assert bool(((dgamma.double() - y[0].double() * x64[0]).abs() <= tol * 40).all())
+    y64 = y.double()
+    want = rs * (y64 - y64.mean() - x64 * (y64 * x64).mean())
+    assert bool(((dx.double() - want).abs() <= U * want.abs() + tol * 7).all())
+    del dgamma, dbeta, dx, y64, want, x64, y
+    K = 20
+    x[0, D - 1], x[0, 5], x[0, D - 2] = 30.0, 30.0, 20.0
+    vals, idx = torch.empty((1, K), device="cuda"), torch.empty((1, K), device="cuda", dtype=torch.int32)
+    B.rn18op_topk_logits(B.RN18_BF16, x, vals, idx, 1, D, D, K, ws_of(B.rn18op_topk_logits_workspace(B.RN18_BF16, 1, D, K)))
+    assert idx[0, :3].tolist() == [5, D - 1, D - 2]
+    v, at = x[0].float().topk(4 * K)
+    ties = sorted(zip((-v).tolist(), at.tolist()))
+    assert v[-1] < v[K - 1] and [(-a, b) for a, b in ties[:K]] == list(zip(vals[0].tolist(), idx[0].tolist()))
+    T = 4.0
+    dz, row, loss = torch.empty_like(x), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    lab = torch.tensor([D - 3], device="cuda", dtype=torch.int32)
+    scale = 2.0 ** 20
+    B.rn18op_distill_loss(B.RN18_BF16, x, vals, idx, lab, None, dz, row, loss, 1, D, D, D, K, T, 0.5, scale,
+                          ws_of(B.rn18op_distill_loss_workspace(B.RN18_BF16, 1, D, K)))
+    z = x[0].double()
+    q = torch.softmax(vals[0].double() / T, 0)
+    i = idx[0].long()
+    want = torch.zeros(D, dtype=torch.float64, device="cuda")
+    value = 0.0
+    for t, w in ((T, 0.5 * T), (1.0, 0.5)):
+        lse = torch.logsumexp(z / t, 0)
+        want += w * torch.exp(z / t - lse)
+        if t == T:
+            want.scatter_add_(0, i, -w * q)
+            value += 0.5 * T * T * (q * (q.log() - z[i] / T + lse)).sum()
+        else:
+            want[D - 3] -= w
+            value += 0.5 * (lse - z[D - 3])
+    want *= scale
+    assert abs(row.item() / value.item() - 1) <= tol
+    assert bool(((dz[0].double() - want).abs() <= U * want.abs() + tol * want.abs()).all())
