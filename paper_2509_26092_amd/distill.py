@@ -3,7 +3,8 @@ a batch, and a student learns from them and the labels.
 
 Two students: the library's own ResNet-18 step (Worker.train_step_distill),
 and TokenStudent, a small network of patches with layer norm over channels,
-whose forward and backward passes call the row operators.
+whose forward and backward passes call the row operators (its products, ReLU
+and means are torch's, as in a network of the user's).
 
     python -m paper_2509_26092_amd.distill --student tokens --steps 50
 """
