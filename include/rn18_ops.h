@@ -79,7 +79,8 @@ int rn18op_maxpool_bwd(int prec, const void* dy, const uint8_t* arg, void* dx, i
 int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* hip_stream);
 
 /* ---- Row operators -------------------------------------------------------
- * Layer norm, a teacher's top logits and the distillation loss work on R rows
+ * Layer norm, RMS norm, dropout, a teacher's top logits and the distillation
+ * loss work on R rows
  * of a matrix whose rows are `ld` elements apart (ld >= the width; any ld, any
  * width from 1 to 2^30). Their tensors of the storage type need only the alignment
  * of one element, their fp32 and int32 arrays that of 4 bytes; rows may be of
@@ -112,6 +113,61 @@ size_t rn18op_layernorm_bwd_workspace(int prec, int64_t R, int D);
 int rn18op_layernorm_bwd(int prec, const void* dy, const void* x, const float* gamma, const float* mean,
                          const float* rstd, void* dx, float* dgamma, float* dbeta, int64_t R, int D, int64_t lddy,
                          int64_t ldx, int64_t lddx, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Dropout of the rows of x, with a residual's addition:
+ *   y = res + m x,  m = keep / (1 - p)
+ * keep(r, j) iff (w >> 8) >= floor(p 2^24), w = word j mod 4 of Philox4x32-10
+ * (Salmon et al., SC'11) with key (seed mod 2^32, seed div 2^32) and counter
+ * (q mod 2^32, q div 2^32, t mod 2^32, t div 2^32), q = r ceil(D/4) + j div 4,
+ * t = step + *step_add mod 2^64, and kept elements are multiplied by
+ * (float)(1 / (1 - p)): rn18_set_dropout's mask where D is a multiple of 4.
+ * No mask is stored: the gradient of x is the same call on dy without res,
+ * that of res is dy. What is dropped is 0 whatever x holds there. res may be
+ * NULL; p in [0, 1). step_add (NULL: 0) points to a 64-bit count on the
+ * device that is read when the kernel runs, so that a replayed graph takes
+ * the step that stands there then. y may be x or res itself. */
+int rn18op_dropout(int prec, const void* x, const void* res, void* y, int64_t R, int D, int64_t ldx, int64_t ldres,
+                   int64_t ldy, float p, uint64_t seed, uint64_t step, const uint64_t* step_add, void* hip_stream);
+
+/* Root-mean-square norm over the D elements of each row, with the branch's
+ * dropout and the residual's addition in the same pass:
+ *   h = res + m x (m as above, 1 for p = 0; rounded to the storage type),
+ *   rstd = 1 / sqrt(sum h^2 / D + eps),  y = h rstd gamma
+ * h is written for the residual stream and the backward pass; the norm takes
+ * it as it is stored. res may be NULL (0), gamma fp32 [D] too (1), rstd fp32
+ * [R] too (in inference); h may be NULL where it would be x itself (no res,
+ * p = 0). h and y may each be x or res, but not the same. The sum of squares
+ * is fp32's: beyond its range (elements from 1.8e19 on) rstd is 0; a row that
+ * holds a NaN gives NaN, and one that holds an infinity NaN there and 0
+ * elsewhere. */
+int rn18op_rmsnorm_fwd(int prec, const void* x, const void* res, const float* gamma, void* h, void* y, float* rstd,
+                       int64_t R, int D, int64_t ldx, int64_t ldres, int64_t ldh, int64_t ldy, float eps, float p,
+                       uint64_t seed, uint64_t step, const uint64_t* step_add, void* hip_stream);
+
+/* The same with y in 8 bits (OCP e4m3, one byte an element, rows ldy8 bytes
+ * apart) and a scale a row, for products in 8 bits:
+ *   a = max(max_j |y_j|, 1e-30),  scale = a / 448,  y8 = e4m3(y / scale)
+ * to nearest even, y in fp32. A row with a NaN in y has a NaN scale and NaN
+ * codes. scale fp32 [R]; y8 overlaps no other tensor. */
+int rn18op_rmsnorm_fwd_q8(int prec, const void* x, const void* res, const float* gamma, void* h, uint8_t* y8,
+                          float* scale, float* rstd, int64_t R, int D, int64_t ldx, int64_t ldres, int64_t ldh,
+                          int64_t ldy8, float eps, float p, uint64_t seed, uint64_t step, const uint64_t* step_add,
+                          void* hip_stream);
+
+/* Its backward pass, from the stored h and rstd:
+ *   g = dy gamma, xh = h rstd,
+ *   dh = rstd (g - xh sum(g xh) / D) + dr,  dx = m dh,
+ *   dgamma = sum over rows of dy xh
+ * dr is the gradient that h receives from the residual stream behind it
+ * (NULL: none); dh is the gradient of res, dx that of x: equal for p = 0, and
+ * either may be NULL. dgamma fp32 [D], overwritten (zeros for R = 0; NULL: not
+ * wanted, and no workspace needed). dh and dx may each be dy, dr or h, but
+ * not the same. p, seed and step as in the forward pass. */
+size_t rn18op_rmsnorm_bwd_workspace(int prec, int64_t R, int D);
+int rn18op_rmsnorm_bwd(int prec, const void* dy, const void* dr, const void* h, const float* gamma, const float* rstd,
+                       void* dh, void* dx, float* dgamma, int64_t R, int D, int64_t lddy, int64_t lddr, int64_t ldh,
+                       int64_t lddh, int64_t lddx, float p, uint64_t seed, uint64_t step, const uint64_t* step_add,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* The K largest of the C logits of each row, 1 <= K <= min(C, 256):
  *   vals fp32 [R][K] in descending order, idx int32 [R][K] their classes
@@ -152,6 +208,52 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
                         const float* row_weight, void* dz, float* row_loss, float* loss, int64_t R, int C,
                         int64_t ldz, int64_t lddz, int K, float temperature, float alpha, float scale,
                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- Linear attention with a decay for each head ---------------------------
+ * A causal mixer of the tokens of B sequences of up to T tokens, H query
+ * heads over Hk key and value heads (H a multiple of Hk; query head h reads
+ * key head h div (H / Hk)), a state S of Dk x Dv for each sequence and query
+ * head:
+ *   S_t = exp(g_h) S_(t-1) + k_t v_t^T,   o_t = scale S_t^T q_t
+ * q [B T][H Dk], k [B T][Hk Dk], v [B T][Hk Dv], o [B T][H Dv]: token t of
+ * sequence b is row b T + t, rows are ld elements apart (any ld from the
+ * width on; elements need only their own alignment, so that all may be parts
+ * of one buffer). log_decay fp32 [H]: g, a constant of the model that no
+ * gradient is taken of; -infinity is a head without memory, and g above 0 a
+ * growing one. lengths int32 [B] on the device (NULL: all T; values are taken
+ * into [0, T]): tokens from a sequence's length on are neither read nor
+ * written. States are fp32 [B][H][Dk][Dv], dense: s0 before the first token
+ * (NULL: zeros), sT after the last (NULL: not wanted; may be s0 itself). Dk
+ * and Dv from 1 to 256, B T H up to 2^31 - 1, B H up to 2^20, T up to 2^26. Sums and states
+ * are fp32; the products of 16-bit types keep the decayed and summed operands
+ * in parts of 8 bits that add up to 16 bits or more, and o is rounded once.
+ * Outputs overlap no input but for sT. Results do not depend on the order in
+ * which blocks run. Workspaces are those of the row operators. */
+size_t rn18op_linattn_fwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
+int rn18op_linattn_fwd(int prec, const void* q, const void* k, const void* v, const float* log_decay,
+                       const int32_t* lengths, const float* s0, void* o, float* sT, int B, int T, int H, int Hk, int Dk,
+                       int Dv, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float scale, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/* Its backward pass, from the forward pass's inputs (dO is `dout`, dS_T the
+ * gradient of sT, NULL: zeros):
+ *   S_t as above,  dq_t = scale S_t dO_t,
+ *   G_t = exp(g) G_(t+1) + scale q_t dO_t^T,  exp(g) G_(length) = dS_T
+ *   dk_t = G_t v_t,  dv_t = G_t^T k_t,  ds0 = exp(g) G_0
+ * dk and dv are added up over the query heads that share a key head (in fp32).
+ * ds0 may be NULL, or dS_T itself. */
+size_t rn18op_linattn_bwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
+int rn18op_linattn_bwd(int prec, const void* q, const void* k, const void* v, const void* dout,
+                       const float* log_decay, const int32_t* lengths, const float* s0, const float* dsT, void* dq,
+                       void* dk, void* dv, float* ds0, int B, int T, int H, int Hk, int Dk, int Dv, int64_t ldq,
+                       int64_t ldk, int64_t ldv, int64_t lddout, int64_t lddq, int64_t lddk, int64_t lddv, float scale,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One token of each of B sequences, for serving: rows are the sequences.
+ * state_out [B][H][Dk][Dv] may be state_in itself. */
+int rn18op_linattn_step(int prec, const void* q, const void* k, const void* v, const float* log_decay,
+                        const float* state_in, void* o, float* state_out, int B, int H, int Hk, int Dk, int Dv,
+                        int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float scale, void* hip_stream);
 
 /* Debugging aids (not part of the training path).
  * rn18_debug_set(ctx, RN18_DBG_STOP_BLOCKS, k): later train steps end their

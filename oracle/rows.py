@@ -1,5 +1,6 @@
-"""Row operators in fp64: layer norm forward and backward, the top logits of
-a row, and the distillation loss with its gradient.
+"""Row operators in fp64: layer norm forward and backward, dropout of rows, RMS
+norm forward and backward, the top logits of a row, and the distillation loss
+with its gradient.
 
 Test infrastructure only (see the package docstring). Each function is the
 textbook definition written out: layer normalisation over the channels of a
@@ -8,6 +9,8 @@ T^2) restricted to the teacher's listed classes, mixed with the labels'
 cross-entropy.
 """
 import numpy as np
+
+from oracle import philox
 
 
 def layernorm_forward(x, gamma, beta, eps):
@@ -31,6 +34,32 @@ def layernorm_backward(dy, x, gamma, mean, rstd):
     g = dy if gamma is None else dy * np.asarray(gamma, np.float64)
     dx = rstd * (g - g.mean(axis=1, keepdims=True) - xh * (g * xh).mean(axis=1, keepdims=True))
     return dx, (dy * xh).sum(axis=0), dy.sum(axis=0)
+
+
+def dropout_factor(seed, step, rows, width, p):
+    """The factor keep / (1 - p) of every element of rows x width: element j of
+    row r draws word j mod 4 of the counter (r ceil(width / 4) + j div 4)."""
+    padded = (width + 3) // 4 * 4
+    keep = philox.dropout_keep(seed, step, rows, padded, p)[:, :width]
+    return keep * philox.dropout_params(p)[1]
+
+
+def rmsnorm_forward(h, gamma, eps):
+    """(y, rstd) of rows h [R][D]; gamma [D] or None."""
+    h = np.asarray(h, np.float64)
+    rstd = 1.0 / np.sqrt((h ** 2).mean(axis=1) + eps)
+    y = h * rstd[:, None]
+    return (y if gamma is None else y * np.asarray(gamma, np.float64)), rstd
+
+
+def rmsnorm_backward(dy, dr, h, gamma, rstd):
+    """(dh, dgamma) from the forward pass's rows and statistic; dr: what else
+    the rows' gradient receives, or None."""
+    dy, h, rstd = (np.asarray(a, np.float64) for a in (dy, h, rstd))
+    xh = h * rstd[:, None]
+    g = dy if gamma is None else dy * np.asarray(gamma, np.float64)
+    dh = rstd[:, None] * (g - xh * (g * xh).mean(axis=1, keepdims=True))
+    return (dh if dr is None else dh + np.asarray(dr, np.float64)), (dy * xh).sum(axis=0)
 
 
 def topk(z, k):

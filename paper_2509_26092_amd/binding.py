@@ -35,6 +35,9 @@ EXPORTED = [
     "rn18_debug_capture", "rn18op_round_bf16", "rn18op_conv2d_wgrad_noalloc_limit", "rn18op_conv2d_wgrad_noalloc",
     "rn18_train_step_distill", "rn18op_layernorm_fwd", "rn18op_layernorm_bwd_workspace", "rn18op_layernorm_bwd",
     "rn18op_topk_logits_workspace", "rn18op_topk_logits", "rn18op_distill_loss_workspace", "rn18op_distill_loss",
+    "rn18op_dropout", "rn18op_rmsnorm_fwd", "rn18op_rmsnorm_fwd_q8", "rn18op_rmsnorm_bwd_workspace",
+    "rn18op_rmsnorm_bwd", "rn18op_linattn_fwd_workspace", "rn18op_linattn_fwd", "rn18op_linattn_bwd_workspace",
+    "rn18op_linattn_bwd", "rn18op_linattn_step",
 ]
 
 
@@ -66,6 +69,7 @@ _I = ctypes.c_int
 _Z = ctypes.c_size_t
 _F = ctypes.c_float
 _L = ctypes.c_int64
+_U = ctypes.c_uint64
 
 
 def lib():
@@ -111,6 +115,18 @@ def lib():
         "rn18op_distill_loss_workspace": (_Z, [_I, _L, _I, _I]),
         "rn18op_distill_loss": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _I, _F, _F, _F, _P, _Z,
                                      _P]),
+        "rn18op_dropout": (_I, [_I, _P, _P, _P, _L, _I, _L, _L, _L, _F, _U, _U, _P, _P]),
+        "rn18op_rmsnorm_fwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _L, _L, _F, _F, _U, _U, _P, _P]),
+        "rn18op_rmsnorm_fwd_q8": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _L, _L, _F, _F, _U, _U, _P,
+                                       _P]),
+        "rn18op_rmsnorm_bwd_workspace": (_Z, [_I, _L, _I]),
+        "rn18op_rmsnorm_bwd": (_I, [_I, _P, _P, _P, _P, _P, _P, _P, _P, _L, _I, _L, _L, _L, _L, _L, _F, _U, _U, _P, _P,
+                                    _Z, _P]),
+        "rn18op_linattn_fwd_workspace": (_Z, [_I] * 7),
+        "rn18op_linattn_fwd": (_I, [_I] + [_P] * 8 + [_I] * 6 + [_L] * 4 + [_F, _P, _Z, _P]),
+        "rn18op_linattn_bwd_workspace": (_Z, [_I] * 7),
+        "rn18op_linattn_bwd": (_I, [_I] + [_P] * 12 + [_I] * 6 + [_L] * 7 + [_F, _P, _Z, _P]),
+        "rn18op_linattn_step": (_I, [_I] + [_P] * 7 + [_I] * 5 + [_L] * 4 + [_F, _P]),
         "rn18_debug_set": (_I, [_P, _I, ctypes.c_long]),
         "rn18_profile_enable": (_I, [_P, _I]),
         "rn18_profile_read": (_I, [_P, ctypes.POINTER(rn18_prof_rec), _I, ctypes.POINTER(_I)]),
@@ -367,6 +383,84 @@ def rn18op_distill_loss(prec, z, t_vals, t_idx, labels, row_weight, dz, row_loss
                                             _arr(row_weight, "float32", "row_weight", R), _ptr(dz), _ptr(row_loss),
                                             _ptr(loss), R, C, ldz, lddz, K, temperature, alpha, scale, *_ws(ws),
                                             _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_dropout(prec, x, res, y, R, D, ldx, ldres, ldy, p, seed, step, step_add=None, stream=None):
+    r = (_lib or lib()).rn18op_dropout(prec, _ptr(x), _ptr(res), _ptr(y), R, D, ldx, ldres, ldy, p, seed, step,
+                                       _arr(step_add, "int64", "step_add", 1), _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_rmsnorm_fwd(prec, x, res, gamma, h, y, rstd, R, D, ldx, ldres, ldh, ldy, eps=1e-5, p=0.0, seed=0, step=0,
+                       step_add=None, stream=None):
+    r = (_lib or lib()).rn18op_rmsnorm_fwd(prec, _ptr(x), _ptr(res), _arr(gamma, "float32", "gamma", D), _ptr(h),
+                                           _ptr(y), _arr(rstd, "float32", "rstd", R), R, D, ldx, ldres, ldh, ldy, eps,
+                                           p, seed, step, _arr(step_add, "int64", "step_add", 1), _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_rmsnorm_fwd_q8(prec, x, res, gamma, h, y8, scale, rstd, R, D, ldx, ldres, ldh, ldy8, eps=1e-5, p=0.0,
+                          seed=0, step=0, step_add=None, stream=None):
+    r = (_lib or lib()).rn18op_rmsnorm_fwd_q8(prec, _ptr(x), _ptr(res), _arr(gamma, "float32", "gamma", D), _ptr(h),
+                                              _ptr(y8), _arr(scale, "float32", "scale", R),
+                                              _arr(rstd, "float32", "rstd", R), R, D, ldx, ldres, ldh, ldy8, eps, p,
+                                              seed, step, _arr(step_add, "int64", "step_add", 1), _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_rmsnorm_bwd_workspace(prec, R, D):
+    return lib().rn18op_rmsnorm_bwd_workspace(prec, R, D)
+
+
+def rn18op_rmsnorm_bwd(prec, dy, dr, h, gamma, rstd, dh, dx, dgamma, R, D, lddy, lddr, ldh, lddh, lddx, p=0.0, seed=0,
+                       step=0, step_add=None, ws=None, stream=None):
+    r = (_lib or lib()).rn18op_rmsnorm_bwd(prec, _ptr(dy), _ptr(dr), _ptr(h), _arr(gamma, "float32", "gamma", D),
+                                           _arr(rstd, "float32", "rstd", R), _ptr(dh), _ptr(dx),
+                                           _arr(dgamma, "float32", "dgamma", D), R, D, lddy, lddr, ldh, lddh, lddx, p,
+                                           seed, step, _arr(step_add, "int64", "step_add", 1), *_ws(ws),
+                                           _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_linattn_fwd_workspace(prec, B, T, H, Hk, Dk, Dv):
+    return lib().rn18op_linattn_fwd_workspace(prec, B, T, H, Hk, Dk, Dv)
+
+
+def rn18op_linattn_fwd(prec, q, k, v, log_decay, lengths, s0, o, sT, B, T, H, Hk, Dk, Dv, ldq, ldk, ldv, ldo, scale,
+                       ws=None, stream=None):
+    n = B * H * Dk * Dv
+    r = (_lib or lib()).rn18op_linattn_fwd(prec, _ptr(q), _ptr(k), _ptr(v), _arr(log_decay, "float32", "log_decay", H),
+                                           _arr(lengths, "int32", "lengths", B), _arr(s0, "float32", "s0", n), _ptr(o),
+                                           _arr(sT, "float32", "sT", n), B, T, H, Hk, Dk, Dv, ldq, ldk, ldv, ldo, scale,
+                                           *_ws(ws), _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_linattn_bwd_workspace(prec, B, T, H, Hk, Dk, Dv):
+    return lib().rn18op_linattn_bwd_workspace(prec, B, T, H, Hk, Dk, Dv)
+
+
+def rn18op_linattn_bwd(prec, q, k, v, dout, log_decay, lengths, s0, dsT, dq, dk, dv, ds0, B, T, H, Hk, Dk, Dv, ldq, ldk,
+                       ldv, lddout, lddq, lddk, lddv, scale, ws=None, stream=None):
+    n = B * H * Dk * Dv
+    r = (_lib or lib()).rn18op_linattn_bwd(prec, _ptr(q), _ptr(k), _ptr(v), _ptr(dout),
+                                           _arr(log_decay, "float32", "log_decay", H),
+                                           _arr(lengths, "int32", "lengths", B), _arr(s0, "float32", "s0", n),
+                                           _arr(dsT, "float32", "dsT", n), _ptr(dq), _ptr(dk), _ptr(dv),
+                                           _arr(ds0, "float32", "ds0", n), B, T, H, Hk, Dk, Dv, ldq, ldk, ldv, lddout,
+                                           lddq, lddk, lddv, scale, *_ws(ws), _stream(stream))
+    return _check(r) if r else r
+
+
+def rn18op_linattn_step(prec, q, k, v, log_decay, state_in, o, state_out, B, H, Hk, Dk, Dv, ldq, ldk, ldv, ldo, scale,
+                        stream=None):
+    n = B * H * Dk * Dv
+    r = (_lib or lib()).rn18op_linattn_step(prec, _ptr(q), _ptr(k), _ptr(v),
+                                            _arr(log_decay, "float32", "log_decay", H),
+                                            _arr(state_in, "float32", "state_in", n), _ptr(o),
+                                            _arr(state_out, "float32", "state_out", n), B, H, Hk, Dk, Dv, ldq, ldk, ldv,
+                                            ldo, scale, _stream(stream))
     return _check(r) if r else r
 
 

@@ -20,6 +20,7 @@
 #include "../../include/rn18.h"
 #include "../../include/rn18_ops.h"
 #include "kernels.h"
+#include "philox.h"
 
 using namespace rn18;
 
@@ -1768,7 +1769,7 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* stream) {
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
-// Row operators: layer norm, top logits, distillation
+// Row operators: layer norm, dropout, RMS norm, top logits, distillation; linear attention
 // ---------------------------------------------------------------------------
 namespace {
 constexpr int64_t kMaxRowElems = (int64_t)1 << 46;   // rows x stride of one tensor
@@ -1844,6 +1845,102 @@ int rn18op_layernorm_bwd(int prec, const void* dy, const void* x, const float* g
   return RN18_OK;
 }
 
+// The dropout of (p, seed, step); *d is left alone for p = 0.
+static int dropout_check(float p, uint64_t seed, uint64_t step, const uint64_t* step_add, Dropout* d) {
+  if (!(p >= 0.f && p < 1.f)) return fail(RN18_EINVAL, "dropout rate must be in [0, 1)");
+  if ((uintptr_t)step_add & 7u) return fail(RN18_EINVAL, "step_add is misaligned");
+  *d = Dropout{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)floor((double)p * 16777216.0),
+               (float)(1.0 / (1.0 - (double)p)), step, step_add};
+  return RN18_OK;
+}
+static int apart_check(const char* a, const void* pa, const char* b, const void* pb) {
+  return pa && pa == pb ? fail(RN18_EINVAL, "%s and %s must not be the same", a, b) : RN18_OK;
+}
+
+int rn18op_dropout(int prec, const void* x, const void* res, void* y, int64_t R, int D, int64_t ldx, int64_t ldres,
+                   int64_t ldy, float p, uint64_t seed, uint64_t step, const uint64_t* step_add, void* stream) {
+  int r;
+  Dropout d;
+  if ((r = row_sizes_check(prec, R, D)) || (r = rows_check(prec, "x", x, R, D, ldx)) ||
+      (res && (r = rows_check(prec, "res", res, R, D, ldres))) || (r = rows_check(prec, "y", y, R, D, ldy)) ||
+      (r = alias_check("y", y, ldy, x, ldx, R)) || (r = alias_check("y", y, ldy, res, ldres, R)) ||
+      (r = dropout_check(p, seed, step, step_add, &d)))
+    return r;
+  LCHK(dropout_rows_launch(prec, x, res, y, R, D, ldx, ldres, ldy, d, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+static int rmsnorm_fwd(int prec, const RmsFwd& a, float p, uint64_t seed, uint64_t step, const uint64_t* step_add,
+                       void* stream) {
+  int r;
+  Dropout d;
+  if ((r = rows_check(prec, "x", a.x, a.R, a.D, a.ldx)) ||
+      (a.res && (r = rows_check(prec, "res", a.res, a.R, a.D, a.ldres))) ||
+      (a.h && (r = rows_check(prec, "h", a.h, a.R, a.D, a.ldh))) || (r = alias_check("h", a.h, a.ldh, a.x, a.ldx, a.R)) ||
+      (r = alias_check("h", a.h, a.ldh, a.res, a.ldres, a.R)) || (r = words_check("gamma", a.gamma, false)) ||
+      (r = words_check("rstd", a.rstd, false)) || (r = dropout_check(p, seed, step, step_add, &d)))
+    return r;
+  if (!(a.eps >= 0.f) || !isfinite(a.eps)) return fail(RN18_EINVAL, "eps must be finite and not negative");
+  if (!a.h && a.R > 0 && (a.res || p > 0.f)) return fail(RN18_EINVAL, "h is NULL beside a residual or dropout");
+  if ((r = apart_check("h", a.h, "y", a.y))) return r;
+  LCHK(rmsnorm_fwd_launch(prec, a, p > 0.f ? &d : nullptr, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+int rn18op_rmsnorm_fwd(int prec, const void* x, const void* res, const float* gamma, void* h, void* y, float* rstd,
+                       int64_t R, int D, int64_t ldx, int64_t ldres, int64_t ldh, int64_t ldy, float eps, float p,
+                       uint64_t seed, uint64_t step, const uint64_t* step_add, void* stream) {
+  int r;
+  if ((r = row_sizes_check(prec, R, D)) || (r = rows_check(prec, "y", y, R, D, ldy)) ||
+      (r = alias_check("y", y, ldy, x, ldx, R)) || (r = alias_check("y", y, ldy, res, ldres, R)))
+    return r;
+  return rmsnorm_fwd(prec, RmsFwd{x, res, gamma, h, y, nullptr, rstd, R, ldx, ldres, ldh, ldy, D, eps}, p, seed, step,
+                     step_add, stream);
+}
+
+int rn18op_rmsnorm_fwd_q8(int prec, const void* x, const void* res, const float* gamma, void* h, uint8_t* y8,
+                          float* scale, float* rstd, int64_t R, int D, int64_t ldx, int64_t ldres, int64_t ldh,
+                          int64_t ldy8, float eps, float p, uint64_t seed, uint64_t step, const uint64_t* step_add,
+                          void* stream) {
+  int r;
+  if ((r = row_sizes_check(prec, R, D))) return r;
+  if (R > 0 && !y8) return fail(RN18_EINVAL, "y8 is NULL");
+  if (ldy8 < D) return fail(RN18_EINVAL, "the row stride of y8 is below its width");
+  if (R > 0 && ldy8 > kMaxRowElems / R) return fail(RN18_EINVAL, "y8 spans more than 2^46 elements");
+  if ((r = words_check("scale", scale, true)) || (r = apart_check("y8", y8, "x", x)) ||
+      (r = apart_check("y8", y8, "res", res)))
+    return r;
+  return rmsnorm_fwd(prec, RmsFwd{x, res, gamma, h, y8, scale, rstd, R, ldx, ldres, ldh, ldy8, D, eps}, p, seed, step,
+                     step_add, stream);
+}
+
+size_t rn18op_rmsnorm_bwd_workspace(int prec, int64_t R, int D) {
+  return row_sizes_check(prec, R, D) ? 0 : rmsnorm_bwd_workspace(prec, R, D);
+}
+
+int rn18op_rmsnorm_bwd(int prec, const void* dy, const void* dr, const void* h, const float* gamma, const float* rstd,
+                       void* dh, void* dx, float* dgamma, int64_t R, int D, int64_t lddy, int64_t lddr, int64_t ldh,
+                       int64_t lddh, int64_t lddx, float p, uint64_t seed, uint64_t step, const uint64_t* step_add,
+                       void* ws, size_t ws_bytes, void* stream) {
+  int r;
+  Dropout d;
+  if ((r = row_sizes_check(prec, R, D)) || (r = rows_check(prec, "dy", dy, R, D, lddy)) ||
+      (dr && (r = rows_check(prec, "dr", dr, R, D, lddr))) || (r = rows_check(prec, "h", h, R, D, ldh)) ||
+      (dh && (r = rows_check(prec, "dh", dh, R, D, lddh))) || (dx && (r = rows_check(prec, "dx", dx, R, D, lddx))) ||
+      (r = words_check("gamma", gamma, false)) || (r = words_check("rstd", rstd, R > 0)) ||
+      (r = words_check("dgamma", dgamma, false)) || (r = apart_check("dh", dh, "dx", dx)) ||
+      (r = alias_check("dh", dh, lddh, dy, lddy, R)) || (r = alias_check("dh", dh, lddh, dr, lddr, R)) ||
+      (r = alias_check("dh", dh, lddh, h, ldh, R)) || (r = alias_check("dx", dx, lddx, dy, lddy, R)) ||
+      (r = alias_check("dx", dx, lddx, dr, lddr, R)) || (r = alias_check("dx", dx, lddx, h, ldh, R)) ||
+      (r = dropout_check(p, seed, step, step_add, &d)))
+    return r;
+  if (R > 0 && !dh && !dx) return fail(RN18_EINVAL, "dh and dx are NULL");
+  if (dgamma && (r = ws_check(ws, ws_bytes, rmsnorm_bwd_workspace(prec, R, D)))) return r;
+  const RmsBwd a{dy, dr, h, gamma, rstd, dh, dx, dgamma, R, lddy, lddr, ldh, lddh, lddx, D};
+  LCHK(rmsnorm_bwd_launch(prec, a, p > 0.f ? &d : nullptr, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
 static int topk_check(int prec, int64_t R, int C, int K) {
   int r = row_sizes_check(prec, R, C);
   if (r) return r;
@@ -1894,6 +1991,98 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
   const DistillArgs a{z, t_vals, t_idx, labels, row_weight, dz, row_loss, R, ldz, lddz, C, K, temperature, alpha,
                       scale, nullptr, nullptr};
   LCHK(distill_launch(prec, a, loss, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+static int linattn_check(int prec, int B, int T, int H, int Hk, int Dk, int Dv) {
+  if (prec != RN18_FP32 && prec != RN18_BF16 && prec != RN18_FP16) return fail(RN18_EINVAL, "bad precision");
+  if (B < 0 || T < 0 || T > 1 << 26) return fail(RN18_EINVAL, "bad number of sequences or tokens");
+  if (H < 1 || Hk < 1 || H % Hk) return fail(RN18_EINVAL, "H must be a positive multiple of Hk");
+  if (Dk < 1 || Dk > 256 || Dv < 1 || Dv > 256) return fail(RN18_EINVAL, "Dk and Dv must be in [1, 256]");
+  if ((int64_t)B * (T > 1 ? T : 1) > INT32_MAX / H) return fail(RN18_EINVAL, "more than 2^31 - 1 heads of tokens");
+  if ((int64_t)B * H > 1 << 20) return fail(RN18_EINVAL, "more than 2^20 heads of sequences");
+  return RN18_OK;
+}
+// The rows of a tensor of `heads` heads of `width` elements.
+static int heads_check(int prec, const char* name, const void* p, int64_t rows, int heads, int width, int64_t ld) {
+  if ((int64_t)heads * width > kMaxWidth) return fail(RN18_EINVAL, "rows of more than 2^30 elements");
+  return rows_check(prec, name, p, rows, heads * width, ld);
+}
+
+size_t rn18op_linattn_fwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv) {
+  return linattn_check(prec, B, T, H, Hk, Dk, Dv) ? 0 : linattn_fwd_workspace(prec, B, T, H, Hk, Dk, Dv);
+}
+
+int rn18op_linattn_fwd(int prec, const void* q, const void* k, const void* v, const float* log_decay,
+                       const int32_t* lengths, const float* s0, void* o, float* sT, int B, int T, int H, int Hk, int Dk,
+                       int Dv, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float scale, void* ws,
+                       size_t ws_bytes, void* stream) {
+  int r = linattn_check(prec, B, T, H, Hk, Dk, Dv);
+  if (r) return r;
+  const int64_t rows = (int64_t)B * T;
+  if ((r = heads_check(prec, "q", q, rows, H, Dk, ldq)) || (r = heads_check(prec, "k", k, rows, Hk, Dk, ldk)) ||
+      (r = heads_check(prec, "v", v, rows, Hk, Dv, ldv)) || (r = heads_check(prec, "o", o, rows, H, Dv, ldo)) ||
+      (r = words_check("log_decay", log_decay, true)) || (r = words_check("lengths", lengths, false)) ||
+      (r = words_check("s0", s0, false)) || (r = words_check("sT", sT, false)) || (r = apart_check("o", o, "q", q)) ||
+      (r = apart_check("o", o, "k", k)) || (r = apart_check("o", o, "v", v)))
+    return r;
+  if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
+  if ((r = ws_check(ws, ws_bytes, linattn_fwd_workspace(prec, B, T, H, Hk, Dk, Dv)))) return r;
+  const LinattnFwd a{q, k, v, log_decay, lengths, s0, o, sT, ldq, ldk, ldv, ldo, B, T, H, Hk, Dk, Dv, scale};
+  LCHK(linattn_fwd_launch(prec, a, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+size_t rn18op_linattn_bwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv) {
+  return linattn_check(prec, B, T, H, Hk, Dk, Dv) ? 0 : linattn_bwd_workspace(prec, B, T, H, Hk, Dk, Dv);
+}
+
+int rn18op_linattn_bwd(int prec, const void* q, const void* k, const void* v, const void* dout,
+                       const float* log_decay, const int32_t* lengths, const float* s0, const float* dsT, void* dq,
+                       void* dk, void* dv, float* ds0, int B, int T, int H, int Hk, int Dk, int Dv, int64_t ldq,
+                       int64_t ldk, int64_t ldv, int64_t lddout, int64_t lddq, int64_t lddk, int64_t lddv, float scale,
+                       void* ws, size_t ws_bytes, void* stream) {
+  int r = linattn_check(prec, B, T, H, Hk, Dk, Dv);
+  if (r) return r;
+  const int64_t rows = (int64_t)B * T;
+  if ((r = heads_check(prec, "q", q, rows, H, Dk, ldq)) || (r = heads_check(prec, "k", k, rows, Hk, Dk, ldk)) ||
+      (r = heads_check(prec, "v", v, rows, Hk, Dv, ldv)) || (r = heads_check(prec, "dout", dout, rows, H, Dv, lddout)) ||
+      (r = heads_check(prec, "dq", dq, rows, H, Dk, lddq)) || (r = heads_check(prec, "dk", dk, rows, Hk, Dk, lddk)) ||
+      (r = heads_check(prec, "dv", dv, rows, Hk, Dv, lddv)) || (r = words_check("log_decay", log_decay, true)) ||
+      (r = words_check("lengths", lengths, false)) || (r = words_check("s0", s0, false)) ||
+      (r = words_check("dsT", dsT, false)) || (r = words_check("ds0", ds0, false)))
+    return r;
+  const struct { const char* name; const void* p; } ins[] = {{"q", q}, {"k", k}, {"v", v}, {"dout", dout}},
+                                                    outs[] = {{"dq", dq}, {"dk", dk}, {"dv", dv}};
+  for (const auto& o : outs) {
+    for (const auto& i : ins)
+      if ((r = apart_check(o.name, o.p, i.name, i.p))) return r;
+    for (const auto& i : outs)
+      if (&o != &i && (r = apart_check(o.name, o.p, i.name, i.p))) return r;
+  }
+  if ((r = apart_check("ds0", ds0, "s0", s0))) return r;
+  if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
+  if ((r = ws_check(ws, ws_bytes, linattn_bwd_workspace(prec, B, T, H, Hk, Dk, Dv)))) return r;
+  const LinattnBwd a{q, k, v, dout, log_decay, lengths, s0, dsT, dq, dk, dv, ds0, ldq, ldk, ldv, lddout, lddq, lddk,
+                     lddv, B, T, H, Hk, Dk, Dv, scale};
+  LCHK(linattn_bwd_launch(prec, a, ws, (hipStream_t)stream));
+  return RN18_OK;
+}
+
+int rn18op_linattn_step(int prec, const void* q, const void* k, const void* v, const float* log_decay,
+                        const float* state_in, void* o, float* state_out, int B, int H, int Hk, int Dk, int Dv,
+                        int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldo, float scale, void* stream) {
+  int r = linattn_check(prec, B, 1, H, Hk, Dk, Dv);
+  if (r) return r;
+  if ((r = heads_check(prec, "q", q, B, H, Dk, ldq)) || (r = heads_check(prec, "k", k, B, Hk, Dk, ldk)) ||
+      (r = heads_check(prec, "v", v, B, Hk, Dv, ldv)) || (r = heads_check(prec, "o", o, B, H, Dv, ldo)) ||
+      (r = words_check("log_decay", log_decay, true)) || (r = words_check("state_in", state_in, B > 0)) ||
+      (r = words_check("state_out", state_out, B > 0)) || (r = apart_check("o", o, "q", q)) ||
+      (r = apart_check("o", o, "k", k)) || (r = apart_check("o", o, "v", v)))
+    return r;
+  if (!isfinite(scale)) return fail(RN18_EINVAL, "scale is not finite");
+  const LinattnFwd a{q, k, v, log_decay, nullptr, state_in, o, state_out, ldq, ldk, ldv, ldo, B, 1, H, Hk, Dk, Dv, scale};
+  LCHK(linattn_step_launch(prec, a, (hipStream_t)stream));
   return RN18_OK;
 }
 

@@ -281,6 +281,65 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
                          const float* rstd, void* dx, float* dgamma, float* dbeta, long R, int D, long lddy, long ldx,
                          long lddx, void* ws, hipStream_t s);
 
+// Sums of the columns of nb partial rows, each n (1 or 2) arrays of D rounded
+// up to 4 columns, added up in a fixed order: a from the first, b from the
+// second array (either may be NULL).
+int column_sums_launch(const float* part, int nb, int D, int n, float* a, float* b, hipStream_t s);
+
+// Dropout and RMS norm of R rows of D elements (see philox.h, rmsnorm.hip).
+struct Dropout;
+int dropout_rows_launch(int prec, const void* x, const void* res, void* y, long R, int D, long ldx, long ldres,
+                        long ldy, const Dropout& d, hipStream_t s);
+struct RmsFwd {
+  const void *x, *res;   // res, h may be NULL
+  const float* gamma;
+  void *h, *y;           // y: the storage type, or e4m3 with a scale a row
+  float *scale, *rstd;   // scale NULL: y in the storage type
+  long R, ldx, ldres, ldh, ldy;
+  int D;
+  float eps;
+};
+int rmsnorm_fwd_launch(int prec, const RmsFwd& a, const Dropout* d, hipStream_t s);
+struct RmsBwd {
+  const void *dy, *dr, *h;   // dr may be NULL
+  const float *gamma, *rstd;
+  void *dh, *dx;             // one of them may be NULL
+  float* dgamma;
+  long R, lddy, lddr, ldh, lddh, lddx;
+  int D;
+};
+size_t rmsnorm_bwd_workspace(int prec, long R, int D);
+int rmsnorm_bwd_launch(int prec, const RmsBwd& a, const Dropout* d, void* ws, hipStream_t s);
+
+// Linear attention with a decay for each head (see linattn.hip).
+struct LinattnFwd {
+  const void *q, *k, *v;
+  const float* log_decay;
+  const int32_t* lengths;   // may be NULL
+  const float* s0;          // may be NULL
+  void* o;
+  float* sT;                // may be NULL
+  long ldq, ldk, ldv, ldo;
+  int B, T, H, Hk, Dk, Dv;
+  float scale;
+};
+size_t linattn_fwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
+int linattn_fwd_launch(int prec, const LinattnFwd& a, void* ws, hipStream_t s);
+int linattn_step_launch(int prec, const LinattnFwd& a, hipStream_t s);
+struct LinattnBwd {
+  const void *q, *k, *v, *dout;
+  const float* log_decay;
+  const int32_t* lengths;
+  const float *s0, *dsT;    // may be NULL
+  void *dq, *dk, *dv;
+  float* ds0;               // may be NULL
+  long ldq, ldk, ldv, lddout, lddq, lddk, lddv;
+  int B, T, H, Hk, Dk, Dv;
+  float scale;
+};
+size_t linattn_bwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
+int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s);
+
 // The K largest logits of R rows over C classes and their classes, in
 // descending order; K at most kTopMax, topk_workspace bytes at ws.
 constexpr int kTopMax = 256;

@@ -19,7 +19,6 @@
 
 #include <algorithm>
 
-#include "kernels.h"
 #include "rows.h"
 
 namespace rn18 {
@@ -29,31 +28,6 @@ namespace {
 inline int ok() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
 // ------------------------------------------------------------------ rows in registers
-template <int VW>
-__device__ inline void load_param(const float* p, int start, float fill, float* v) {
-#pragma unroll
-  for (int j = 0; j < VW; ++j) v[j] = fill;
-  if (p) __builtin_memcpy(v, p + start, VW * 4);
-}
-
-// Where a lane's E chunks start (e * L + l of the row), whether it has the
-// last of them (the others are whole), and its element of the tail. L >= 8
-// lanes where there is a tail.
-template <int VW, int L, int E>
-struct Span {
-  int start[E], tail;
-  bool last, has_tail;
-  __device__ Span(int l, int D) {
-    const int nch = D / VW;
-#pragma unroll
-    for (int e = 0; e < E; ++e) start[e] = (e * L + l) * VW;
-    last = (E - 1) * L + l < nch;
-    if (!last) start[E - 1] = 0;
-    tail = nch * VW + l;
-    has_tail = tail < D;
-  }
-};
-
 // A block takes NT / L * U rows at a time, gridDim.x blocks after another;
 // the next rows are loaded while the current ones are worked on.
 template <typename T, int L, int E, int U>
@@ -403,7 +377,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void ln_bwd_kernel(const T* dy, 
 // threads are counted in 32 bits, which 2^27 columns would pass.
 constexpr int kSumCols = 1 << 26;
 __global__ __launch_bounds__(1024) void ln_param_sum_kernel(const float* __restrict__ part, int nb, int D, int Dp,
-                                                            int c0, float* __restrict__ dgamma,
+                                                            long ldp, int c0, float* __restrict__ dgamma,
                                                             float* __restrict__ dbeta) {
   __shared__ float sh[128][33], sh2[32][33];
   const int cl = threadIdx.x & 7, rg = threadIdx.x >> 3;
@@ -413,7 +387,7 @@ __global__ __launch_bounds__(1024) void ln_param_sum_kernel(const float* __restr
     const float* p = part + (long)blockIdx.y * Dp + c;
 #pragma unroll 4
     for (int b = rg; b < nb; b += 128) {
-      const float4 v = *(const float4*)(p + (long)b * 2 * Dp);
+      const float4 v = *(const float4*)(p + b * ldp);
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
   }
@@ -507,17 +481,7 @@ __global__ __launch_bounds__(256) void ln_bwd_short_kernel(const T* dy, const T*
 
 // ------------------------------------------------------------------ rows beyond a block's registers
 // A block of 1024 threads per row reads it three times.
-__device__ inline float block_sum1024(float v, float* sh) {
-  v = group_sum<64>(v);
-  __syncthreads();   // earlier readers of sh are done
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = sh[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) t += sh[i];
-  return t;
-}
-
+// A block of 1024 threads per row reads it three times.
 template <typename T>
 __global__ __launch_bounds__(1024) void ln_fwd_long_kernel(const T* x, const float* __restrict__ gamma,
                                                            const float* __restrict__ beta, T* y,
@@ -637,39 +601,6 @@ __global__ __launch_bounds__(256) void ln_param_long_kernel(const T* __restrict_
 }
 
 // ------------------------------------------------------------------ choice of kernel
-enum LnPath { LN_SHORT, LN_TILE, LN_LONG };
-
-// The lanes L and chunks E of a row of D elements: one chunk per lane up to a
-// wave, then up to `max_e` chunks per lane of a wave, and of blocks of up to
-// 1024 threads.
-LnPath ln_tile(int prec, int D, int max_e, int* L, int* E) {
-  const int vw = prec_vw(prec);
-  if (D < vw) return LN_SHORT;
-  const int nch = D / vw;
-  *E = 1;
-  *L = D % vw ? 8 : 1;   // (a lane each for the tail)
-  while (*L < 64 && *L < nch) *L *= 2;
-  if (nch <= 64) return LN_TILE;
-  for (int l = 64; l <= 1024; l *= l == 64 ? 4 : 2)
-    if (nch <= l * max_e) {
-      *L = l;
-      *E = ceil_div(nch, l);
-      // (32 columns a lane beside gamma and beta do not fit in a lane's 128
-      // registers: 2000x32768 bf16 forward 91 us, as a long row 85)
-      return l == 1024 && *E * vw > 24 ? LN_LONG : LN_TILE;
-    }
-  return LN_LONG;
-}
-
-// Blocks for `units` pieces of work, `per_cu` blocks a compute unit at most,
-// all with the same number of pieces but for the last.
-int even_grid(long units, int per_cu) {
-  const long most = (long)per_cu * plan_cus();
-  if (units <= most) return (int)std::max(1l, units);
-  const long each = (units + most - 1) / most;
-  return (int)((units + each - 1) / each);
-}
-
 int ln_fwd_per_cu(int L) { return L > 256 ? 4096 / L : 16; }
 
 template <typename T, int L, int E, int U, typename... A>
@@ -713,9 +644,9 @@ int fwd_tile(int L, int E, long R, hipStream_t s, A... a) {
 }
 
 // Blocks of the backward pass, one partial row each.
-int bwd_grid(LnPath path, int L, long R, int D) {
-  if (path == LN_SHORT) return even_grid((R + 255) / 256, 2);
-  if (path == LN_LONG) return (int)std::max(1l, std::min(R, 8l * plan_cus() / ceil_div(D, 256)));
+int bwd_grid(RowPath path, int L, long R, int D) {
+  if (path == ROW_SHORT) return even_grid((R + 255) / 256, 2);
+  if (path == ROW_LONG) return (int)std::max(1l, std::min(R, 8l * plan_cus() / ceil_div(D, 256)));
   const int G = L > 256 ? 1 : 256 / L;
   return even_grid((R + G - 1) / G, L > 256 ? 1024 / L : L < 64 ? 3 : 2);
 }
@@ -764,21 +695,30 @@ int bwd_tile(int L, int E, int grid, hipStream_t s, A... a) {
 constexpr int kFwdMaxE = 4;
 int bwd_max_e(int prec) { return 16 / prec_vw(prec); }   // 16 columns a lane: their sums and gamma in 48 registers
 
-int row_grid(long R) { return (int)std::min(R, 65536l); }
-
 }  // namespace
+
+int column_sums_launch(const float* part, int nb, int D, int n, float* a, float* b, hipStream_t s) {
+  const int Dp = (D + 3) & ~3;
+  for (int c0 = 0; c0 < Dp; c0 += kSumCols) {
+    hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(std::min(Dp - c0, kSumCols), 32), n), dim3(1024), 0, s, part,
+                       nb, D, Dp, (long)n * Dp, c0, a, b);
+    const int r = ok();
+    if (r) return r;
+  }
+  return 0;
+}
 
 int layernorm_fwd_launch(int prec, const void* x, const float* gamma, const float* beta, void* y, float* mean,
                          float* rstd, long R, int D, long ldx, long ldy, float eps, hipStream_t s) {
   if (R <= 0) return 0;
   int L = 0, E = 0;
-  const LnPath path = ln_tile(prec, D, kFwdMaxE, &L, &E);
+  const RowPath path = row_tile(prec, D, kFwdMaxE, &L, &E);
   return with_prec(prec, [&](auto tag) {
     using T = decltype(tag);
     const T* xt = (const T*)x;
     T* yt = (T*)y;
-    if (path == LN_TILE) return fwd_tile<T>(L, E, R, s, xt, gamma, beta, yt, mean, rstd, R, D, ldx, ldy, eps);
-    if (path == LN_SHORT)
+    if (path == ROW_TILE) return fwd_tile<T>(L, E, R, s, xt, gamma, beta, yt, mean, rstd, R, D, ldx, ldy, eps);
+    if (path == ROW_SHORT)
       hipLaunchKernelGGL(ln_fwd_short_kernel<T>, dim3(row_grid((R + 255) / 256)), dim3(256), 0, s, xt, gamma, beta, yt,
                          mean, rstd, R, D, ldx, ldy, eps);
     else
@@ -801,7 +741,7 @@ static bool ln_bwd_small(int prec, long R, int D) {
 size_t layernorm_bwd_workspace(int prec, long R, int D) {
   if (R <= 0) return 0;
   int L = 0, E = 0;
-  const LnPath path = ln_tile(prec, D, bwd_max_e(prec), &L, &E);
+  const RowPath path = row_tile(prec, D, bwd_max_e(prec), &L, &E);
   return (size_t)bwd_grid(path, L, R, D) * 2 * ((D + 3) & ~3) * 4;
 }
 
@@ -809,21 +749,21 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
                          const float* rstd, void* dx, float* dgamma, float* dbeta, long R, int D, long lddy, long ldx,
                          long lddx, void* ws, hipStream_t s) {
   int L = 0, E = 0;
-  const LnPath path = ln_tile(prec, D, bwd_max_e(prec), &L, &E);
+  const RowPath path = row_tile(prec, D, bwd_max_e(prec), &L, &E);
   const bool params = dgamma || dbeta;
   const int grid = R > 0 ? bwd_grid(path, L, R, D) : 0;
   // (dx in place of dy or x would be written while the column sums read them)
-  const bool small = params && R > 0 && path == LN_TILE && L < 1024 && dx != dy && dx != x && ln_bwd_small(prec, R, D);
+  const bool small = params && R > 0 && path == ROW_TILE && L < 1024 && dx != dy && dx != x && ln_bwd_small(prec, R, D);
   const LnParamOut po{params && !small ? (float*)ws : nullptr, (D + 3) & ~3, grid, dgamma, dbeta};
   if (R > 0) {
     const int r = with_prec(prec, [&](auto tag) {
       using T = decltype(tag);
       const T *dyt = (const T*)dy, *xt = (const T*)x;
       T* dxt = (T*)dx;
-      if (path == LN_TILE)
+      if (path == ROW_TILE)
         return bwd_tile<T>(L, E, small ? grid + ceil_div(D, 32) : grid, s, dyt, xt, gamma, mean, rstd, dxt, po, R, D,
                            lddy, ldx, lddx);
-      if (path == LN_SHORT) {
+      if (path == ROW_SHORT) {
         hipLaunchKernelGGL(ln_bwd_short_kernel<T>, dim3(grid), dim3(256), 0, s, dyt, xt, gamma, mean, rstd, dxt, po, R,
                            D, lddy, ldx, lddx);
         return ok();
@@ -837,13 +777,7 @@ int layernorm_bwd_launch(int prec, const void* dy, const void* x, const float* g
     });
     if (r) return r;
   }
-  if (params && !small)
-    for (int c0 = 0; c0 < po.Dp; c0 += kSumCols) {
-      hipLaunchKernelGGL(ln_param_sum_kernel, dim3(ceil_div(std::min(po.Dp - c0, kSumCols), 32), 2), dim3(1024), 0, s,
-                         (const float*)ws, grid, D, po.Dp, c0, dgamma, dbeta);
-      const int r = ok();
-      if (r) return r;
-    }
+  if (params && !small) return column_sums_launch((const float*)ws, grid, D, 2, dgamma, dbeta, s);
   return 0;
 }
 

@@ -7,6 +7,7 @@
 #include <math.h>
 
 #include "kernels.h"
+#include "philox.h"
 #include "pool.h"
 
 namespace rn18 {
@@ -166,25 +167,6 @@ __global__ __launch_bounds__(256) void repack_tiled_kernel(const float* __restri
 }
 
 // ------------------------------------------------------------------ dropout
-// Philox4x32-10 (Salmon et al., SC'11): ten rounds of two 32x32 -> 64-bit
-// products mixed with the other counter words and the key, the key bumped by
-// the Weyl constants between rounds.
-__device__ inline void philox4x32_10(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    if (r) {
-      k0 += 0x9E3779B9u;
-      k1 += 0xBB67AE85u;
-    }
-    const uint64_t p0 = (uint64_t)0xD2511F53u * c[0], p1 = (uint64_t)0xCD9E8D57u * c[2];
-    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c[1] ^ k0, n2 = (uint32_t)(p0 >> 32) ^ c[3] ^ k1;
-    c[0] = n0;
-    c[1] = (uint32_t)p1;
-    c[2] = n2;
-    c[3] = (uint32_t)p0;
-  }
-}
-
 // In-place dropout of n fp32 values, four per counter: group q draws one
 // Philox output (counter (q, step), key seed); value 4q + w is kept iff the
 // top 24 bits of word w are >= thresh, and kept values are scaled. A ragged

@@ -1,8 +1,10 @@
-// Device helpers of the row operators (layer norm, top logits, distillation):
-// 16-byte chunks of rows that may start at any element, and reductions over
-// groups of lanes.
+// Helpers of the row operators (layer norm, RMS norm, dropout, top logits,
+// distillation): 16-byte chunks of rows that may start at any element,
+// reductions over groups of lanes, and the lanes and blocks that rows get.
 #pragma once
-#include "common.h"
+#include <algorithm>
+
+#include "kernels.h"
 
 namespace rn18 {
 
@@ -143,5 +145,81 @@ __device__ inline void row_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
+
+// The sum over a block of 1024 threads.
+__device__ inline float block_sum1024(float v, float* sh) {
+  v = group_sum<64>(v);
+  __syncthreads();   // earlier readers of sh are done
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = sh[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) t += sh[i];
+  return t;
+}
+
+// VW parameters of a row from `start` on, `fill` without them.
+template <int VW>
+__device__ inline void load_param(const float* p, int start, float fill, float* v) {
+#pragma unroll
+  for (int j = 0; j < VW; ++j) v[j] = fill;
+  if (p) __builtin_memcpy(v, p + start, VW * 4);
+}
+
+// Where a lane's E chunks start (e * L + l of the row), whether it has the
+// last of them (the others are whole), and its element of the tail. L >= 8
+// lanes where there is a tail.
+template <int VW, int L, int E>
+struct Span {
+  int start[E], tail;
+  bool last, has_tail;
+  __device__ Span(int l, int D) {
+    const int nch = D / VW;
+#pragma unroll
+    for (int e = 0; e < E; ++e) start[e] = (e * L + l) * VW;
+    last = (E - 1) * L + l < nch;
+    if (!last) start[E - 1] = 0;
+    tail = nch * VW + l;
+    has_tail = tail < D;
+  }
+};
+
+// ------------------------------------------------------------------ lanes and blocks
+enum RowPath { ROW_SHORT, ROW_TILE, ROW_LONG };
+
+// The lanes L and chunks E of a row of D elements: one chunk per lane up to a
+// wave, then up to `max_e` chunks per lane of a wave, and of blocks of up to
+// 1024 threads.
+inline RowPath row_tile(int prec, int D, int max_e, int* L, int* E) {
+  const int vw = prec_vw(prec);
+  if (D < vw) return ROW_SHORT;
+  const int nch = D / vw;
+  *E = 1;
+  *L = D % vw ? 8 : 1;   // (a lane each for the tail)
+  while (*L < 64 && *L < nch) *L *= 2;
+  if (nch <= 64) return ROW_TILE;
+  for (int l = 64; l <= 1024; l *= l == 64 ? 4 : 2)
+    if (nch <= l * max_e) {
+      *L = l;
+      *E = ceil_div(nch, l);
+      // (32 columns a lane beside gamma and beta do not fit in a lane's 128
+      // registers: 2000x32768 bf16 forward 91 us, as a long row 85)
+      return l == 1024 && *E * vw > 24 ? ROW_LONG : ROW_TILE;
+    }
+  return ROW_LONG;
+}
+
+// Blocks for `units` pieces of work, `per_cu` blocks a compute unit at most,
+// all with the same number of pieces but for the last.
+inline int even_grid(long units, int per_cu) {
+  const long most = (long)per_cu * plan_cus();
+  if (units <= most) return (int)std::max(1l, units);
+  const long each = (units + most - 1) / most;
+  return (int)((units + each - 1) / each);
+}
+
+inline int row_grid(long R) { return (int)std::min(R, 65536l); }
+
+inline int launched() { return hipGetLastError() == hipSuccess ? 0 : -4; }
 
 }  // namespace rn18
