@@ -337,3 +337,26 @@ def test_offsets_beyond_32_bits():
     B.rn18op_linattn_fwd(P, q, q, q, g, None, None, o, None, *sizes, ld, ld, ld, D, 1.0, ws)
     B.rn18op_linattn_fwd(P, a, a, a, g, None, None, o2, None, *sizes, D, D, D, D, 1.0, ws)
     assert torch.equal(o, o2)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_what_a_token_holds_reaches_no_earlier_one(prec, what, value):
+    """A NaN or an infinity of token 37, in a chunk with earlier tokens: those
+    keep their outputs; from there on the head's are not finite (q: that token's alone)."""
+    import torch
+    c = Case(prec, 2, 100, 2, 2, 32, 48, None, True)
+    clean = c.fwd()[0].view(2, 100, 2, 48)
+    t = c.dev[what].view(2, 100, 2, -1)
+    t[0, 37, 1, 3] = value
+    o = c.fwd()[0].view(2, 100, 2, 48)
+    assert torch.equal(o[1], clean[1]) and torch.equal(o[0, :, 0], clean[0, :, 0])
+    near(f64(o[0, :37, 1]), f64(clean[0, :37, 1]), 2 * U[prec] * np.abs(f64(clean[0, :37, 1])) + acc(prec, 100) * 10, "o")
+    bad = ~torch.isfinite(o[0, :, 1])
+    if what == "q":
+        assert bad[37].all() and torch.equal(o[0, 38:, 1], clean[0, 38:, 1])
+    elif what == "k":
+        assert bad[37:].all()
+    else:
+        assert bad[37:, 3].all() and torch.equal(o[0, :, 1, 16:], clean[0, :, 1, 16:])
