@@ -1,0 +1,580 @@
+// The chunked form of linear attention with a decay for each head: operands,
+// kernel and choice of kernel (linattn.hip has the operators made of it; each
+// storage type's kernels are compiled apart).
+#pragma once
+#include <math.h>
+
+#include <type_traits>
+
+#include "rows.h"
+
+namespace rn18 {
+
+// One operand: rows ld elements apart, head h of the pass at column
+// (h / group) * width.
+struct Operand {
+  const void* p;
+  long ld;
+  int group;
+};
+// A pass: for the tokens in order (rev: from the last to the first)
+//   S <- exp(g) S + kv_scale k v^T (M x N),  out = out_scale S^T q
+// rev takes the decay behind a token instead of before it:
+//   S' = S + kv_scale k v^T,  out = out_scale S'^T q,  S <- exp(g) S'
+// s_in and s_out hold element (m, n) of a head's state at m * s_m + n * s_n.
+struct Core {
+  Operand q, k, v;
+  void* out;
+  long ldo;
+  int out_f32;   // out is fp32 [tokens][H][N] whatever the storage type
+  const float* log_decay;
+  const int32_t* lengths;
+  const float* s_in;
+  float* s_out;
+  int s_m, s_n;
+  int B, T, H, M, N, rev;
+  float out_scale, kv_scale;
+};
+
+// A call's split: segments of a sequence, chunks of a segment.
+struct Split {
+  int nseg, chunks;
+};
+// What the segments before each one leave of the state, in place of their sums.
+int segments_launch(const Core& c, float* states, int nseg, int tokens, hipStream_t s);
+int chunks_launch_fp32(const Core& c, const Split& p, float* states, hipStream_t s);
+int chunks_launch_bf16(const Core& c, const Split& p, float* states, hipStream_t s);
+int chunks_launch_fp16(const Core& c, const Split& p, float* states, hipStream_t s);
+
+namespace {
+
+// Tokens of sequence b.
+__device__ inline int seq_len(const Core& c, int b) {
+  return c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
+}
+
+// ------------------------------------------------------------------ chunks on the matrix units
+// A sequence is taken in chunks of 32 tokens. With X the state before a chunk
+// of n tokens and i, j its tokens,
+//   out_i = decay^(i + 1 - rev) X^T q_i + sum_(j <= i) decay^(i - j) (q_i . k_j) v_j
+//   X <- decay^n X + sum_j decay^(n - 1 + rev - j) k_j v_j^T
+// (the second terms of both with kv_scale). No power is above one for a decay
+// below one. A wave takes 16 NT columns of a head's state through the chunks:
+// X stays in the accumulators of the matrix units, and so do the scores: what
+// comes out of one product, rows 4 (lane / 16) + 0..3 of each 16, is an operand
+// of the next whose inner index goes over these rows, if the other operand is
+// read in the same order. Only q, k and v pass through LDS, q and k once for
+// the W waves of a block, which share a head. The next chunk's rows are loaded
+// into registers meanwhile.
+//
+// Matrix operands in 16 bits are bf16, which has fp32's range: fp16 inputs are
+// held as two parts each (exact), what is computed in fp32 (X, the scores, the
+// decayed v) as two or three. Products of parts below 2^-16 of the result are
+// left out, for the state 2^-24.
+
+// A lane's operand of one step over KB of the inner index, in NP parts: places
+// 4 (lane / 16) + 0..3 of the first and of the second 16 in 16 bits, of 16 in
+// fp32 (four steps of the unit).
+template <int P> struct Frag { uint4 p[P]; };
+
+template <int P> struct Ops16 {
+  typedef bf16_t lds_t;
+  static constexpr int NP = P, KB = 32, EV = 8;
+  typedef Frag<P> In;
+  typedef Frag<2> Two;
+  typedef Frag<3> Three;
+  __device__ static inline bf16x8_t v8(const uint4& q) { return __builtin_bit_cast(bf16x8_t, q); }
+  // The products of part i of a and part j of b with i + j < LIM, the smallest first.
+  template <int LIM, int A, int B>
+  __device__ static inline void mma(floatx4_t& acc, const Frag<A>& a, const Frag<B>& b) {
+#pragma unroll
+    for (int i = A - 1; i >= 0; --i)
+#pragma unroll
+      for (int j = B - 1; j >= 0; --j)
+        if (i + j < LIM) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8(a.p[i]), v8(b.p[j]), acc, 0, 0, 0);
+  }
+  // The leading parts of two values, which keep the rest.
+  __device__ static inline uint32_t take(float& a, float& b) {
+    const uint32_t h = f2bf2(a, b);
+    a -= __builtin_bit_cast(float, h << 16);
+    b -= __builtin_bit_cast(float, h & 0xffff0000u);
+    return h;
+  }
+  template <int N>
+  __device__ static inline Frag<N> parts(float (&v)[8]) {
+    Frag<N> f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = take(v[2 * i], v[2 * i + 1]);
+      f.p[n] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return f;
+  }
+  __device__ static inline void values(const In& f, float (&v)[8]) {
+    unpack<bf16_t>(f.p[0], v);
+    if constexpr (P > 1) {
+      float t[8];
+      unpack<bf16_t>(f.p[1], t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += t[i];
+    }
+  }
+};
+struct Ops32 {
+  typedef float lds_t;
+  static constexpr int NP = 1, KB = 16, EV = 4;
+  typedef Frag<1> In;
+  typedef Frag<1> Two;
+  typedef Frag<1> Three;
+  template <int LIM>
+  __device__ static inline void mma(floatx4_t& acc, const In& a, const In& b) {
+    const floatx4_t x = __builtin_bit_cast(floatx4_t, a.p[0]), y = __builtin_bit_cast(floatx4_t, b.p[0]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[r], y[r], acc, 0, 0, 0);
+  }
+  template <int N>
+  __device__ static inline In parts(float (&v)[4]) {
+    return In{{pack<float>(v)}};
+  }
+  __device__ static inline void values(const In& f, float (&v)[4]) { unpack<float>(f.p[0], v); }
+};
+template <typename T> struct OpsOf { typedef Ops32 type; };
+template <> struct OpsOf<bf16_t> { typedef Ops16<1> type; };
+template <> struct OpsOf<f16_t> { typedef Ops16<2> type; };
+
+typedef short v4i16_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char_t;
+
+constexpr int kChunk = 32;
+
+template <typename T, int MP, int NT, int W>
+struct Tile {
+  typedef typename OpsOf<T>::type O;
+  typedef typename O::lds_t L;
+  static constexpr int NP = O::NP, NB = 16 * NT * W, PAD = 16 / (int)sizeof(L);
+  static constexpr int LDM = MP + PAD, LDN = NB + PAD;              // (rows 4 banks further each)
+  static constexpr int SQ = kChunk * LDM, SV = kChunk * LDN;        // of one part
+  static constexpr int OFF_K = NP * SQ, OFF_V = 2 * NP * SQ;
+  static constexpr int BYTES = (OFF_V + NP * SV) * (int)sizeof(L);
+  static constexpr int WAVES = MP * NT > 256 ? 1 : 2;               // of a SIMD: X is MP NT / 4 registers
+  static_assert(BYTES <= 163840 && BYTES % 16 == 0, "LDS");
+};
+
+// The 16 bytes of a row at p, its column `col`; zeros for columns from `width`
+// on, and where the row is not there. A partial last chunk is
+// read from before its place and shifted. (No branch stands around a load: the
+// compiler would wait there for each.)
+template <typename T, int WIDTHS>
+__device__ inline uint4 load_part(const T* p, int col, int width, bool there) {
+  constexpr int VW = TT<T>::VW;
+  if (WIDTHS == 2) {
+    T e[VW];
+#pragma unroll
+    for (int j = 0; j < VW; ++j) e[j] = *(there && col + j < width ? p + j : (const T*)&kNoChunk);
+    uint4 q;
+    __builtin_memcpy(&q, e, 16);
+    return q;
+  }
+  const bool in = there && col < width;
+  if (WIDTHS == 0) return load_chunk(in ? p : (const T*)&kNoChunk);
+  const int over = max(col + VW - width, 0);
+  const uint4 q = load_chunk(in ? p - over : (const T*)&kNoChunk);
+  const int s = 8 * (int)sizeof(T) * over & 127;
+  const uint64_t lo = q.x | (uint64_t)q.y << 32, hi = q.z | (uint64_t)q.w << 32;
+  const uint64_t l2 = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo, h2 = s >= 64 ? 0 : hi >> s;
+  return make_uint4((uint32_t)l2, (uint32_t)(l2 >> 32), (uint32_t)h2, (uint32_t)(h2 >> 32));
+}
+
+// A chunk of 16 bytes into LDS: its parts, `step` elements apart.
+template <typename T>
+__device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const uint4& q) {
+  if constexpr (OpsOf<T>::type::NP == 1) {
+    *(uint4*)p = q;
+  } else {
+    float v[8];
+    unpack<T>(q, v);
+    const auto f = OpsOf<T>::type::template parts<2>(v);
+    *(uint4*)p = f.p[0];
+    *(uint4*)(p + step) = f.p[1];
+  }
+}
+
+// WIDTHS 0: M and N are whole chunks of 16 bytes, 1: a chunk at least each, 2: one
+// of them is less.
+template <typename T, int MP, int NT, int W, int WIDTHS, bool SUMS>
+__global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Core c, float* seg_states,
+                                                                                           int nseg, int chunks, int nb_n) {
+  typedef Tile<T, MP, NT, W> TI;
+  typedef typename OpsOf<T>::type O;
+  typedef typename O::lds_t L;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int C = kChunk, CT = C / 16, VW = TT<T>::VW, MT = MP / 16, KB = O::KB, KT = KB / 16, NP = O::NP;
+  constexpr int PER_M = MP / VW, PER_N = TI::NB / VW, ROWS_M = 64 * W / PER_M, ROWS_N = 64 * W / PER_N;
+  constexpr int NQ = C / ROWS_M, NV = C / ROWS_N;
+  static_assert(ROWS_M * PER_M == 64 * W && ROWS_N * PER_N == 64 * W && NQ * ROWS_M == C && NV * ROWS_N == C, "loads");
+  __shared__ uint4 smem[TI::BYTES / 16];
+  L* const sQ = (L*)smem;
+  L* const sK = sQ + TI::OFF_K;
+  L* const sV = sQ + TI::OFF_V;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i0 = lane & 15,
+            g = lane >> 4;
+  // neighbours on an XCD: a head's segments, its column blocks, the heads
+  const int segs = SUMS ? nseg - 1 : nseg, id = xcd_remap(blockIdx.x, gridDim.x);
+  const int seg = id % segs, nb = id / segs % nb_n, bh = id / segs / nb_n, b = bh / c.H, h = bh - b * c.H;
+  const int len = seq_len(c, b), t_first = seg * chunks * C, total = min(max(len - t_first, 0), chunks * C);
+  const float g2 = c.log_decay[h] * kLog2e;
+  auto pw = [&](int n) { return n <= 0 ? 1.f : __builtin_amdgcn_exp2f((float)n * g2); };
+  const int n_wave = nb * TI::NB + w * 16 * NT;   // the wave's columns from here on
+  const bool works = n_wave < c.N;
+  // Column of place x of tile nt: two tiles take turns of four, so that a lane
+  // ends up with eight neighbours of an output row.
+  auto col_of = [](int nt, int x) { return 32 * (nt / 2) + 8 * (x >> 2) + 4 * (nt & 1) + (x & 3); };
+
+  floatx4_t X[MT][NT];   // rows 16 mt + 4 g + r, column col_of(nt, i0)
+  {
+    const bool stored = !SUMS && nseg > 1;
+    const float* src = stored ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_in + (long)bh * c.M * c.N;
+    const int s_m = stored ? c.N : c.s_m, s_n = stored ? 1 : c.s_n;
+    const bool any = !SUMS && (stored || c.s_in);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int m = 16 * mt + 4 * g + r, n = n_wave + col_of(nt, i0);
+          X[mt][nt][r] = any && m < c.M && n < c.N ? src[(long)m * s_m + (long)n * s_n] : 0.f;
+        }
+  }
+
+  // A thread's chunks of 16 bytes of an operand: ROWS_M or ROWS_N tokens apart.
+  const long dir = c.rev ? -1 : 1, row0 = (long)b * c.T + (c.rev ? len - 1 - t_first : t_first);
+  uint4 rq[SUMS ? 1 : NQ], rk[NQ], rv[NV];
+  const int im = tid / PER_M, in_ = tid / PER_N, colm = tid % PER_M * VW, coln = tid % PER_N * VW;
+  auto place = [&](const Operand& x, int width, int i, int col) {
+    return (const T*)x.p + (row0 + dir * i) * x.ld + (long)(h / x.group) * width + col;
+  };
+  const T *pq = SUMS ? nullptr : place(c.q, c.M, im, colm), *pk = place(c.k, c.M, im, colm),
+          *pv = place(c.v, c.N, in_, nb * TI::NB + coln);
+  const long sq = dir * c.q.ld, sk = dir * c.k.ld, sv = dir * c.v.ld;   // a token's step
+  auto fetch = [&](int left) __attribute__((always_inline)) {   // the next chunk, of which `left` tokens are there
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
+      const bool there = im + s * ROWS_M < left;
+      if (!SUMS) rq[SUMS ? 0 : s] = load_part<T, WIDTHS>(pq + s * ROWS_M * sq, colm, c.M, there);
+      rk[s] = load_part<T, WIDTHS>(pk + s * ROWS_M * sk, colm, c.M, there);
+    }
+#pragma unroll
+    for (int s = 0; s < NV; ++s)
+      rv[s] = load_part<T, WIDTHS>(pv + s * ROWS_N * sv, nb * TI::NB + coln, c.N, in_ + s * ROWS_N < left);
+    if (!SUMS) pq += C * sq;
+    pk += C * sk;
+    pv += C * sv;
+  };
+
+  // operands from LDS: of a row, and of a column at place i0 of its tile
+  auto frag_row = [&](const L* base, int row, int k0) {
+    typename O::In f;
+    const L* at = base + (row + i0) * TI::LDM + k0 + 4 * g;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      if constexpr (F32) {
+        f.p[p] = *(const uint4*)at;
+      } else {
+        const uint2 x = *(const uint2*)(at + p * TI::SQ), y = *(const uint2*)(at + p * TI::SQ + 16);
+        f.p[p] = make_uint4(x.x, x.y, y.x, y.y);
+      }
+    }
+    return f;
+  };
+  // `col` and `spread`: 16 columns in a row, or by fours 8 apart
+  auto frag_col = [&](const L* base, int ld, int part, int row, int col, int spread) {
+    typename O::In f;
+    if constexpr (F32) {
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = base[(row + 4 * g + r) * ld + col + spread * (i0 >> 2) + (i0 & 3)];
+      f.p[0] = pack<float>(v);
+    } else {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const L* at = base + p * part + (row + 4 * g + (i0 >> 2)) * ld + col + spread * (i0 & 3);
+        auto tr = [](const L* a) {
+          return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               (__attribute__((address_space(3))) v4i16_t*)(lds_char_t*)a));
+        };
+        const uint2 x = tr(at), y = tr(at + 16 * ld);
+        f.p[p] = make_uint4(x.x, x.y, y.x, y.y);
+      }
+    }
+    return f;
+  };
+
+  // powers of the decay that serve every chunk: of a score in a diagonal tile
+  // and in the one below, of a token's place, and of what is left of a chunk
+  // behind a token (anew for a partial last chunk)
+  float diag[4], below[4], up[CT], tail[C / KB][O::EV], less;
+  if (!SUMS) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      diag[r] = i0 < 4 * g + r ? 0.f : pw(i0 - 4 * g - r) * c.kv_scale;
+      below[r] = pw(16 + i0 - 4 * g - r) * c.kv_scale;
+    }
+#pragma unroll
+    for (int it = 0; it < CT; ++it) up[it] = pw(16 * it + i0 + 1 - c.rev);
+  }
+  auto tails = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jb = 0; jb < C / KB; ++jb)
+#pragma unroll
+      for (int e = 0; e < O::EV; ++e)
+        tail[jb][e] = pw(n - 1 + c.rev - (jb * KB + 16 * (e >> 2) + 4 * g + (e & 3))) * c.kv_scale;
+    less = expm1f((float)n * c.log_decay[h]);   // decay^n - 1: exact near 1, where many chunks multiply
+  };
+  tails(C);
+  const int col_out = n_wave + 8 * g;
+  char* po = (char*)c.out + (c.out_f32 ? (((row0 + dir * i0) * c.H + h) * c.N + col_out) * 4
+                                       : ((row0 + dir * i0) * c.ldo + (long)h * c.N + col_out) * (long)sizeof(T));
+  const long so = dir * (c.out_f32 ? (long)c.H * c.N * 4 : c.ldo * (long)sizeof(T));
+
+  if (total > 0) fetch(total);
+  for (int left = total; left > 0; left -= C, po += C * so) {
+    if (left < C) tails(left);
+    __syncthreads();   // the last chunk is read
+#pragma unroll
+    for (int s = 0; s < NQ; ++s) {
+      const int at = (im + s * ROWS_M) * TI::LDM + colm;
+      if (!SUMS) put<T>(sQ + at, TI::SQ, rq[SUMS ? 0 : s]);
+      put<T>(sK + at, TI::SQ, rk[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < NV; ++s) put<T>(sV + (in_ + s * ROWS_N) * TI::LDN + coln, TI::SV, rv[s]);
+    __syncthreads();
+    if (left > C) fetch(left - C);
+    if (!works) continue;
+
+    floatx4_t out[CT][NT], P[CT][CT];   // out^T: rows columns, columns tokens; P^T[it][jt]: rows j, columns i
+    if constexpr (!SUMS) {
+#pragma unroll
+      for (int it = 0; it < CT; ++it) {
+#pragma unroll
+        for (int jt = 0; jt < CT; ++jt) P[it][jt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) out[it][nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int kb = 0; kb < MP / KB; ++kb) {
+        typename O::In q[CT];
+        typename O::Two A[NT];
+#pragma unroll
+        for (int it = 0; it < CT; ++it) q[it] = frag_row(sQ, 16 * it, kb * KB);
+#pragma unroll
+        for (int jt = 0; jt < CT; ++jt) {
+          const auto k = frag_row(sK, 16 * jt, kb * KB);
+#pragma unroll
+          for (int it = jt; it < CT; ++it) O::template mma<2>(P[it][jt], k, q[it]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[O::EV];
+#pragma unroll
+          for (int e = 0; e < O::EV; ++e) x[e] = X[kb * KT + e / 4][nt][e % 4];
+          A[nt] = O::template parts<2>(x);
+#pragma unroll
+          for (int it = 0; it < CT; ++it) O::template mma<2>(out[it][nt], A[nt], q[it]);
+        }
+      }
+#pragma unroll
+      for (int it = 0; it < CT; ++it) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          P[it][it][r] = i0 < 4 * g + r ? 0.f : P[it][it][r] * diag[r];
+          if (it > 0) P[it][0][r] *= below[r];
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) out[it][nt] *= up[it];
+      }
+    }
+
+    // the state behind the chunk
+    typename O::In V[C / KB][NT];
+    float bad = 0.f;   // NaN if one of the chunk's v is not finite
+#pragma unroll
+    for (int jb = 0; jb < C / KB; ++jb)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        V[jb][nt] = frag_col(sV, TI::LDN, TI::SV, jb * KB, w * 16 * NT + col_of(nt, 0), 8);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) X[mt][nt][r] = fmaf(X[mt][nt][r], less, X[mt][nt][r]);
+#pragma unroll
+    for (int jb = 0; jb < C / KB; ++jb) {
+      typename O::In K[MT > 4 ? 1 : MT];   // few rows: their operands once for all columns, otherwise the other way round
+      typename O::Three D[MT > 4 ? NT : 1];
+      if (MT <= 4)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) K[MT > 4 ? 0 : mt] = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float v[O::EV];
+        O::values(V[jb][nt], v);
+#pragma unroll
+        for (int e = 0; e < O::EV; ++e) {
+          bad = fmaf(v[e], 0.f, bad);
+          v[e] *= tail[jb][e];
+        }
+        D[MT > 4 ? nt : 0] = O::template parts<3>(v);
+        if (MT <= 4)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) O::template mma<3>(X[mt][nt], K[MT > 4 ? 0 : mt], D[0]);
+      }
+      if (MT > 4)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const auto k = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) O::template mma<3>(X[mt][nt], k, D[MT > 4 ? nt : 0]);
+        }
+    }
+
+    if constexpr (!SUMS) {
+      // the sums within the chunk
+      if (__builtin_expect(!__any(bad != 0.f), 1)) {
+#pragma unroll
+        for (int it = 0; it < CT; ++it)
+#pragma unroll
+          for (int jb = 0; jb <= it / KT; ++jb) {
+            float p[O::EV];
+#pragma unroll
+            for (int e = 0; e < O::EV; ++e) p[e] = P[it][jb * KT + e / 4][e % 4];
+            const auto f = O::template parts<2>(p);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O::template mma<2>(out[it][nt], V[jb][nt], f);
+          }
+      } else {
+        // a NaN or an infinity of a later token must not meet an earlier
+        // one's zero score: one term after the other
+#pragma unroll
+        for (int it = 0; it < CT; ++it)
+#pragma unroll
+          for (int jt = 0; jt <= it; ++jt)
+#pragma unroll 1
+            for (int jg = 0; jg < 4; ++jg)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int j = 16 * jt + 4 * jg + r;
+                const float p = __shfl(P[it][jt][r], 16 * jg + i0);
+                if (j <= 16 * it + i0)
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                      float v = 0.f;
+#pragma unroll
+                      for (int q = NP - 1; q >= 0; --q)
+                        v += TT<L>::to_f(sV[q * TI::SV + j * TI::LDN + w * 16 * NT + col_of(nt, 4 * g + x)]);
+                      out[it][nt][x] = fmaf(p, v, out[it][nt][x]);
+                    }
+              }
+      }
+#pragma unroll
+      for (int it = 0; it < CT; ++it) {
+        if (16 * it + i0 >= left) continue;
+        char* row = po + 16 * it * so;
+#pragma unroll
+        for (int np = 0; np < NT / 2; ++np) {
+          float v[8];
+#pragma unroll
+          for (int x = 0; x < 8; ++x) v[x] = out[it][2 * np + x / 4][x % 4] * c.out_scale;
+          const int rest = c.N - col_out - 32 * np;
+          if (c.out_f32) {
+            float* o = (float*)row + 32 * np;
+            if (rest >= 8) {
+              __builtin_memcpy(o, v, 32);
+            } else {
+#pragma unroll
+              for (int x = 0; x < 7; ++x)
+                if (x < rest) o[x] = v[x];
+            }
+          } else {
+            T* o = (T*)row + 32 * np;
+            T e[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) e[x] = TT<T>::from_f(v[x]);
+            if (rest >= 8) {
+              __builtin_memcpy(o, e, sizeof(e));
+            } else {
+#pragma unroll
+              for (int x = 0; x < 7; ++x)
+                if (x < rest) o[x] = e[x];
+            }
+          }
+        }
+      }
+    }
+  }
+
+  if (!works || (!SUMS && (!c.s_out || seg != nseg - 1))) return;
+  float* to = SUMS ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_out + (long)bh * c.M * c.N;
+  const int s_m = SUMS ? c.N : c.s_m, s_n = SUMS ? 1 : c.s_n;
+  int m0 = 4 * g;   // (where elements lie is found again, not kept from the start)
+  asm volatile("" : "+v"(m0));
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int m = 16 * mt + m0 + r, n = n_wave + col_of(nt, i0);
+        if (m < c.M && n < c.N) to[(long)m * s_m + (long)n * s_n] = X[mt][nt][r];
+      }
+}
+
+template <typename T, int MP, int NT, int W, int WIDTHS>
+int chunk_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
+  const int heads = c.B * c.H, nb = ceil_div(c.N, 16 * NT * W);
+  if (p.nseg > 1) {
+    hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), dim3(heads * nb * (p.nseg - 1)), dim3(64 * W), 0,
+                       s, c, states, p.nseg, p.chunks, nb);
+    const int r = segments_launch(c, states, p.nseg, p.chunks * kChunk, s);
+    if (r) return r;
+  }
+  hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), dim3(heads * nb * p.nseg), dim3(64 * W), 0, s, c,
+                     states, p.nseg, p.chunks, nb);
+  return launched();
+}
+
+// Waves of a block by the columns of the state, 64 a wave where it has up to
+// 128 rows in 16 bits, otherwise 32 (its accumulators leave no room for more).
+template <typename T, int WIDTHS>
+int widths_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
+  constexpr bool F32 = sizeof(T) == 4;
+  auto waves = [&](auto rows) {
+    constexpr int MP = decltype(rows)::value, NT = F32 || MP > 128 ? 2 : 4, ONE = 64 / (16 * NT);
+    // (for widths below a chunk of 16 bytes, M or N is small)
+    if (c.N <= 64) return chunk_launch<T, MP, NT, ONE, WIDTHS>(c, p, states, s);
+    if constexpr (WIDTHS < 2 || MP == 64)
+      return c.N <= 128 ? chunk_launch<T, MP, NT, 2 * ONE, WIDTHS>(c, p, states, s)
+                        : chunk_launch<T, MP, NT, 4 * ONE, WIDTHS>(c, p, states, s);
+    return -1;
+  };
+  if (c.M <= 64) return waves(std::integral_constant<int, 64>());
+  if (c.M <= 128) return waves(std::integral_constant<int, 128>());
+  return waves(std::integral_constant<int, 256>());
+}
+
+template <typename T>
+int chunks_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
+  constexpr int VW = TT<T>::VW;
+  if (c.M < VW || c.N < VW) return widths_launch<T, 2>(c, p, states, s);
+  return c.M % VW || c.N % VW ? widths_launch<T, 1>(c, p, states, s) : widths_launch<T, 0>(c, p, states, s);
+}
+
+}  // namespace
+
+}  // namespace rn18

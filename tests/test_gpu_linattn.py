@@ -352,11 +352,18 @@ def test_what_a_token_holds_reaches_no_earlier_one(prec, what, value):
     t[0, 37, 1, 3] = value
     o = c.fwd()[0].view(2, 100, 2, 48)
     assert torch.equal(o[1], clean[1]) and torch.equal(o[0, :, 0], clean[0, :, 0])
-    near(f64(o[0, :37, 1]), f64(clean[0, :37, 1]), 2 * U[prec] * np.abs(f64(clean[0, :37, 1])) + acc(prec, 100) * 10, "o")
+    # in the chunk of the token, terms may be added up in another order: both
+    # results are within the bound of the exact one, so within two of each other
+    args = [np.abs(c.np[n]) for n in "qkv"]
+    size = linattn.forward(*args, c.g, None, np.abs(c.s0), c.scale)[0][0, :, 1]
+    ref = f64(clean[0, :, 1])
+    two = 2 * (U[prec] * np.abs(ref) * (1 + U[prec]) + acc(prec, 100) * size)
+    near(f64(o[0, :37, 1]), ref[:37], two[:37], "o")
     bad = ~torch.isfinite(o[0, :, 1])
     if what == "q":
         assert bad[37].all() and torch.equal(o[0, 38:, 1], clean[0, 38:, 1])
     elif what == "k":
         assert bad[37:].all()
     else:
-        assert bad[37:, 3].all() and torch.equal(o[0, :, 1, 16:], clean[0, :, 1, 16:])
+        assert bad[37:, 3].all()
+        near(f64(o[0, :, 1, 4:]), ref[:, 4:], two[:, 4:], "other columns")
