@@ -39,9 +39,11 @@ struct Core {
 // A call's split: segments of a sequence, chunks of a segment.
 struct Split {
   int nseg, chunks;
+  int s_m, s_n;   // element (m, n) of a segment's state
+  bool there;     // another pass has left the segments' states already
 };
 // What the segments before each one leave of the state, in place of their sums.
-int segments_launch(const Core& c, float* states, int nseg, int tokens, hipStream_t s);
+int segments_launch(const Core& c, float* states, const Split& p, hipStream_t s);
 int chunks_launch_fp32(const Core& c, const Split& p, float* states, hipStream_t s);
 int chunks_launch_bf16(const Core& c, const Split& p, float* states, hipStream_t s);
 int chunks_launch_fp16(const Core& c, const Split& p, float* states, hipStream_t s);
@@ -112,6 +114,28 @@ template <int P> struct Ops16 {
     }
     return f;
   }
+  // x, or NaN if one of the operand's values is not finite (products with 0).
+  __device__ static inline float not_finite(const In& f, float x) {
+    const uint32_t w[4] = {f.p[0].x, f.p[0].y, f.p[0].z, f.p[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w[i]), bf16x2_t{(__bf16)0.f, (__bf16)0.f}, x, false);
+    return x;
+  }
+  // Zeros in place of what is not finite.
+  __device__ static inline void clean(In& f) {
+    auto word = [](uint32_t& w) {
+      if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+      if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+    };
+#pragma unroll
+    for (int n = 0; n < P; ++n) {
+      word(f.p[n].x);
+      word(f.p[n].y);
+      word(f.p[n].z);
+      word(f.p[n].w);
+    }
+  }
   __device__ static inline void values(const In& f, float (&v)[8]) {
     unpack<bf16_t>(f.p[0], v);
     if constexpr (P > 1) {
@@ -137,6 +161,21 @@ struct Ops32 {
   template <int N>
   __device__ static inline In parts(float (&v)[4]) {
     return In{{pack<float>(v)}};
+  }
+  __device__ static inline float not_finite(const In& f, float x) {
+    const floatx4_t v = __builtin_bit_cast(floatx4_t, f.p[0]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = fmaf(v[i], 0.f, x);
+    return x;
+  }
+  __device__ static inline void clean(In& f) {
+    auto word = [](uint32_t& w) {
+      if ((w & 0x7f800000u) == 0x7f800000u) w = 0;
+    };
+    word(f.p[0].x);
+    word(f.p[0].y);
+    word(f.p[0].z);
+    word(f.p[0].w);
   }
   __device__ static inline void values(const In& f, float (&v)[4]) { unpack<float>(f.p[0], v); }
 };
@@ -205,15 +244,16 @@ __device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const ui
 // of them is less.
 template <typename T, int MP, int NT, int W, int WIDTHS, bool SUMS>
 __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Core c, float* seg_states,
-                                                                                           int nseg, int chunks, int nb_n) {
+                                                                                           Split p, int nb_n) {
+  const int nseg = p.nseg, chunks = p.chunks;
   typedef Tile<T, MP, NT, W> TI;
   typedef typename OpsOf<T>::type O;
   typedef typename O::lds_t L;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int C = kChunk, CT = C / 16, VW = TT<T>::VW, MT = MP / 16, KB = O::KB, KT = KB / 16, NP = O::NP;
   constexpr int PER_M = MP / VW, PER_N = TI::NB / VW, ROWS_M = 64 * W / PER_M, ROWS_N = 64 * W / PER_N;
-  constexpr int NQ = C / ROWS_M, NV = C / ROWS_N;
-  static_assert(ROWS_M * PER_M == 64 * W && ROWS_N * PER_N == 64 * W && NQ * ROWS_M == C && NV * ROWS_N == C, "loads");
+  constexpr int NQ = ROWS_M > C ? 1 : C / ROWS_M, NV = C / ROWS_N;
+  static_assert(ROWS_M * PER_M == 64 * W && ROWS_N * PER_N == 64 * W && (NQ * ROWS_M == C || NQ == 1) && NV * ROWS_N == C, "loads");
   __shared__ uint4 smem[TI::BYTES / 16];
   L* const sQ = (L*)smem;
   L* const sK = sQ + TI::OFF_K;
@@ -230,13 +270,14 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   const bool works = n_wave < c.N;
   // Column of place x of tile nt: two tiles take turns of four, so that a lane
   // ends up with eight neighbours of an output row.
+  static_assert(NT % 2 == 0, "pairs of tiles");
   auto col_of = [](int nt, int x) { return 32 * (nt / 2) + 8 * (x >> 2) + 4 * (nt & 1) + (x & 3); };
 
   floatx4_t X[MT][NT];   // rows 16 mt + 4 g + r, column col_of(nt, i0)
   {
     const bool stored = !SUMS && nseg > 1;
     const float* src = stored ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_in + (long)bh * c.M * c.N;
-    const int s_m = stored ? c.N : c.s_m, s_n = stored ? 1 : c.s_n;
+    const int s_m = stored ? p.s_m : c.s_m, s_n = stored ? p.s_n : c.s_n;
     const bool any = !SUMS && (stored || c.s_in);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -262,7 +303,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   auto fetch = [&](int left) __attribute__((always_inline)) {   // the next chunk, of which `left` tokens are there
 #pragma unroll
     for (int s = 0; s < NQ; ++s) {
-      const bool there = im + s * ROWS_M < left;
+      const bool there = im + s * ROWS_M < (ROWS_M > C ? min(left, C) : left);
       if (!SUMS) rq[SUMS ? 0 : s] = load_part<T, WIDTHS>(pq + s * ROWS_M * sq, colm, c.M, there);
       rk[s] = load_part<T, WIDTHS>(pk + s * ROWS_M * sk, colm, c.M, there);
     }
@@ -315,15 +356,16 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   // powers of the decay that serve every chunk: of a score in a diagonal tile
   // and in the one below, of a token's place, and of what is left of a chunk
   // behind a token (anew for a partial last chunk)
+  const float scale = c.kv_scale * c.out_scale;
   float diag[4], below[4], up[CT], tail[C / KB][O::EV], less;
   if (!SUMS) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      diag[r] = i0 < 4 * g + r ? 0.f : pw(i0 - 4 * g - r) * c.kv_scale;
-      below[r] = pw(16 + i0 - 4 * g - r) * c.kv_scale;
+      diag[r] = i0 < 4 * g + r ? 0.f : pw(i0 - 4 * g - r) * scale;
+      below[r] = pw(16 + i0 - 4 * g - r) * scale;
     }
 #pragma unroll
-    for (int it = 0; it < CT; ++it) up[it] = pw(16 * it + i0 + 1 - c.rev);
+    for (int it = 0; it < CT; ++it) up[it] = pw(16 * it + i0 + 1 - c.rev) * c.out_scale;
   }
   auto tails = [&](int n) __attribute__((always_inline)) {
 #pragma unroll
@@ -346,6 +388,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 #pragma unroll
     for (int s = 0; s < NQ; ++s) {
       const int at = (im + s * ROWS_M) * TI::LDM + colm;
+      if (ROWS_M > C && im >= C) continue;   // (few rows for many threads)
       if (!SUMS) put<T>(sQ + at, TI::SQ, rq[SUMS ? 0 : s]);
       put<T>(sK + at, TI::SQ, rk[s]);
     }
@@ -424,10 +467,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
         float v[O::EV];
         O::values(V[jb][nt], v);
 #pragma unroll
-        for (int e = 0; e < O::EV; ++e) {
-          bad = fmaf(v[e], 0.f, bad);
-          v[e] *= tail[jb][e];
-        }
+        for (int e = 0; e < O::EV; ++e) v[e] *= tail[jb][e];
+        bad = O::not_finite(V[jb][nt], bad);
         D[MT > 4 ? nt : 0] = O::template parts<3>(v);
         if (MT <= 4)
 #pragma unroll
@@ -443,45 +484,39 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
     }
 
     if constexpr (!SUMS) {
-      // the sums within the chunk
-      if (__builtin_expect(!__any(bad != 0.f), 1)) {
+      // the sums within the chunk. (A NaN or an infinity of a later token must
+      // not meet an earlier one's zero score: it is taken out, and makes the
+      // column's results NaN from its token on.)
+      const bool any_bad = __any(bad != 0.f);
+      if (__builtin_expect(any_bad, 0))
 #pragma unroll
-        for (int it = 0; it < CT; ++it)
+        for (int jb = 0; jb < C / KB; ++jb)
 #pragma unroll
-          for (int jb = 0; jb <= it / KT; ++jb) {
-            float p[O::EV];
+          for (int nt = 0; nt < NT; ++nt) O::clean(V[jb][nt]);
 #pragma unroll
-            for (int e = 0; e < O::EV; ++e) p[e] = P[it][jb * KT + e / 4][e % 4];
-            const auto f = O::template parts<2>(p);
+      for (int it = 0; it < CT; ++it)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) O::template mma<2>(out[it][nt], V[jb][nt], f);
-          }
-      } else {
-        // a NaN or an infinity of a later token must not meet an earlier
-        // one's zero score: one term after the other
+        for (int jb = 0; jb <= it / KT; ++jb) {
+          float p[O::EV];
 #pragma unroll
-        for (int it = 0; it < CT; ++it)
+          for (int e = 0; e < O::EV; ++e) p[e] = P[it][jb * KT + e / 4][e % 4];
+          const auto f = O::template parts<2>(p);
 #pragma unroll
-          for (int jt = 0; jt <= it; ++jt)
+          for (int nt = 0; nt < NT; ++nt) O::template mma<2>(out[it][nt], V[jb][nt], f);
+        }
+      if (__builtin_expect(any_bad, 0))
 #pragma unroll 1
-            for (int jg = 0; jg < 4; ++jg)
+        for (int j = 0; j < C; ++j)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int j = 16 * jt + 4 * jg + r;
-                const float p = __shfl(P[it][jt][r], 16 * jg + i0);
-                if (j <= 16 * it + i0)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                  for (int nt = 0; nt < NT; ++nt)
+            for (int x = 0; x < 4; ++x) {
+              const float v = TT<L>::to_f(sV[j * TI::LDN + w * 16 * NT + col_of(nt, 4 * g + x)]);
+              if (v * 0.f != 0.f)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                      float v = 0.f;
-#pragma unroll
-                      for (int q = NP - 1; q >= 0; --q)
-                        v += TT<L>::to_f(sV[q * TI::SV + j * TI::LDN + w * 16 * NT + col_of(nt, 4 * g + x)]);
-                      out[it][nt][x] = fmaf(p, v, out[it][nt][x]);
-                    }
-              }
-      }
+                for (int it = 0; it < CT; ++it)
+                  if (j <= 16 * it + i0) out[it][nt][x] = __builtin_nanf("");
+            }
 #pragma unroll
       for (int it = 0; it < CT; ++it) {
         if (16 * it + i0 >= left) continue;
@@ -490,12 +525,12 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
         for (int np = 0; np < NT / 2; ++np) {
           float v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = out[it][2 * np + x / 4][x % 4] * c.out_scale;
+          for (int x = 0; x < 8; ++x) v[x] = out[it][2 * np + x / 4][x % 4];
           const int rest = c.N - col_out - 32 * np;
           if (c.out_f32) {
             float* o = (float*)row + 32 * np;
             if (rest >= 8) {
-              __builtin_memcpy(o, v, 32);
+              __builtin_memcpy(o, v, sizeof(v));
             } else {
 #pragma unroll
               for (int x = 0; x < 7; ++x)
@@ -521,7 +556,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 
   if (!works || (!SUMS && (!c.s_out || seg != nseg - 1))) return;
   float* to = SUMS ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_out + (long)bh * c.M * c.N;
-  const int s_m = SUMS ? c.N : c.s_m, s_n = SUMS ? 1 : c.s_n;
+  const int s_m = SUMS ? p.s_m : c.s_m, s_n = SUMS ? p.s_n : c.s_n;
   int m0 = 4 * g;   // (where elements lie is found again, not kept from the start)
   asm volatile("" : "+v"(m0));
 #pragma unroll
@@ -538,29 +573,31 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 template <typename T, int MP, int NT, int W, int WIDTHS>
 int chunk_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
   const int heads = c.B * c.H, nb = ceil_div(c.N, 16 * NT * W);
-  if (p.nseg > 1) {
+  if (p.nseg > 1 && !p.there) {
     hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), dim3(heads * nb * (p.nseg - 1)), dim3(64 * W), 0,
-                       s, c, states, p.nseg, p.chunks, nb);
-    const int r = segments_launch(c, states, p.nseg, p.chunks * kChunk, s);
+                       s, c, states, p, nb);
+    const int r = segments_launch(c, states, p, s);
     if (r) return r;
   }
   hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), dim3(heads * nb * p.nseg), dim3(64 * W), 0, s, c,
-                     states, p.nseg, p.chunks, nb);
+                     states, p, nb);
   return launched();
 }
 
-// Waves of a block by the columns of the state, 64 a wave where it has up to
-// 128 rows in 16 bits, otherwise 32 (its accumulators leave no room for more).
+// A wave takes 32 columns of the state: 64 were slower (83 us in place of 73 at
+// 256x196 tokens, 8 heads of 64, bf16, and 571 of 472 at 1x65537, 16 heads of
+// 128: too few waves beside the vector units' work on X), and 16 too (90, 658:
+// every wave computes the scores).
 template <typename T, int WIDTHS>
 int widths_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
-  constexpr bool F32 = sizeof(T) == 4;
   auto waves = [&](auto rows) {
-    constexpr int MP = decltype(rows)::value, NT = F32 || MP > 128 ? 2 : 4, ONE = 64 / (16 * NT);
+    constexpr int MP = decltype(rows)::value;
     // (for widths below a chunk of 16 bytes, M or N is small)
-    if (c.N <= 64) return chunk_launch<T, MP, NT, ONE, WIDTHS>(c, p, states, s);
+    if (c.N <= 64) return chunk_launch<T, MP, 2, 2, WIDTHS>(c, p, states, s);
     if constexpr (WIDTHS < 2 || MP == 64)
-      return c.N <= 128 ? chunk_launch<T, MP, NT, 2 * ONE, WIDTHS>(c, p, states, s)
-                        : chunk_launch<T, MP, NT, 4 * ONE, WIDTHS>(c, p, states, s);
+      // (eight waves of 256 rows would not fit in the registers)
+      return c.N <= 128 || MP > 128 ? chunk_launch<T, MP, 2, 4, WIDTHS>(c, p, states, s)
+                                    : chunk_launch<T, MP, 2, (MP > 128 ? 4 : 8), WIDTHS>(c, p, states, s);
     return -1;
   };
   if (c.M <= 64) return waves(std::integral_constant<int, 64>());

@@ -16,20 +16,28 @@ namespace {
 // launch leaves what each segment (but the last) adds to the state, this one
 // turns these sums into the states that the segments start from, element by
 // element in order, and a last one takes the segments from there.
-__global__ __launch_bounds__(256) void linattn_segments_kernel(Core c, float* seg_states, int nseg, int tokens) {
+__global__ __launch_bounds__(256) void linattn_segments_kernel(Core c, float* seg_states, Split p, int tokens) {
+  constexpr int U = 8;   // sums loaded at a time
   const int per = c.M * c.N, e = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y, b = bh / c.H;
   if (e >= per) return;
   const int len = seq_len(c, b), m = e / c.N, n = e - m * c.N;
   const float g = c.log_decay[bh - b * c.H];
   float x = c.s_in ? c.s_in[(long)bh * per + (long)m * c.s_m + (long)n * c.s_n] : 0.f;
-  float* p = seg_states + (long)bh * nseg * per + e;
-  for (int s = 0; s < nseg - 1; ++s, p += per) {
-    const int k = min(max(len - s * tokens, 0), tokens);
-    const float add = *p;
-    *p = x;
-    if (k > 0) x = fmaf(x, expm1f((float)k * g), x) + add;
+  const float whole = expm1f((float)tokens * g);
+  float* at = seg_states + (long)bh * p.nseg * per + (long)m * p.s_m + (long)n * p.s_n;
+  for (int s = 0; s < p.nseg; s += U) {
+    float add[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) add[u] = s + u < p.nseg - 1 ? at[(long)u * per] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= p.nseg) break;
+      at[(long)u * per] = x;
+      const int k = min(max(len - (s + u) * tokens, 0), tokens);
+      if (k > 0) x = fmaf(x, k == tokens ? whole : expm1f((float)k * g), x) + add[u];
+    }
+    at += (long)U * per;
   }
-  *p = x;
 }
 
 // The gradients of query heads that share a key head, added up in the order
@@ -110,24 +118,34 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
   }
 }
 
-// Segments of a call: enough waves for the chip where there are few heads, but
-// no segment below eight chunks.
-Split split_of(int B, int T, int H, int N) {
+// Segments of a call: two waves for each SIMD, as many as fit there, where there
+// are few heads; up to 8192 tokens twice as many, which evens out sequences of
+// other lengths (6 ragged ones of up to 4095, 8 heads of 96, fp16 backward: 541
+// us, 592 without; but 1x65537, 16 heads of 128: 472 with twice as many, whose
+// states are then a sixth of the traffic, and 451 without). No segment is below
+// eight chunks. The same for a state and its transpose.
+Split split_of(int B, int T, int H, int M, int N) {
   const int all = std::max(1, ceil_div(T, kChunk));
-  const long waves = std::max(1l, (long)B * H * ceil_div(N, 64)), want = 8l * plan_cus();
-  const long nseg = std::max(1l, 2 * waves >= want ? 1 : std::min((want + waves - 1) / waves, (long)all / 8));
+  const long units = std::max(1l, (long)B * H * ceil_div(std::max(M, N), 64)), want = (all <= 256 ? 8l : 4l) * plan_cus();
+  const long nseg = std::max(1l, units >= 2l * plan_cus() ? 1 : std::min((want + units - 1) / units, (long)all / 8));
   const int chunks = ceil_div(all, nseg);
-  return Split{ceil_div(all, chunks), chunks};
+  return Split{ceil_div(all, chunks), chunks, N, 1, false};
 }
 size_t split_bytes(int B, int T, int H, int M, int N) {
-  const Split p = split_of(B, T, H, N);
+  const Split p = split_of(B, T, H, M, N);
   return p.nseg > 1 ? (size_t)B * H * p.nseg * M * N * 4 : 0;
 }
 
-// `states`: split_bytes of the pass.
-int core_launch(int prec, const Core& c, float* states, hipStream_t s) {
+// `states`: split_bytes of the pass; `there`: the pass before, on the state's
+// transpose, has left its segments' states in them.
+int core_launch(int prec, const Core& c, float* states, hipStream_t s, bool there = false) {
   if (c.B <= 0) return 0;
-  const Split p = split_of(c.B, c.T, c.H, c.N);
+  Split p = split_of(c.B, c.T, c.H, c.M, c.N);
+  if (there) {
+    p.s_m = 1;
+    p.s_n = c.M;
+    p.there = true;
+  }
   switch (prec) {
     case PREC_F32: return chunks_launch_fp32(c, p, states, s);
     case PREC_BF16: return chunks_launch_bf16(c, p, states, s);
@@ -149,9 +167,9 @@ int group_sum_launch(int prec, const float* part, void* out, long ldo, const Lin
 
 }  // namespace
 
-int segments_launch(const Core& c, float* states, int nseg, int tokens, hipStream_t s) {
+int segments_launch(const Core& c, float* states, const Split& p, hipStream_t s) {
   hipLaunchKernelGGL(linattn_segments_kernel, dim3(ceil_div((long)c.M * c.N, 256), c.B * c.H), dim3(256), 0, s, c, states,
-                     nseg, tokens);
+                     p, p.chunks * kChunk);
   return launched();
 }
 
@@ -190,7 +208,8 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   const int G = a.H / a.Hk;
   float *part = (float*)ws, *states = (float*)((char*)ws + group_bytes(a.B, a.T, a.H, a.Hk, a.Dk, a.Dv));
   const Operand q{a.q, a.ldq, 1}, k{a.k, a.ldk, G}, v{a.v, a.ldv, G}, d{a.dout, a.lddout, 1};
-  // dq and dk: on the state's transpose, whose elements are taken the other way round
+  // dq and dk: on the state's transpose, whose elements are taken the other way
+  // round; dv goes with dk's segments
   int r = core_launch(prec, Core{d, v, k, a.dq, a.lddq, 0, a.log_decay, a.lengths, a.s0, nullptr, 1, a.Dv, a.B, a.T,
                                  a.H, a.Dv, a.Dk, 0, a.scale, 1.f}, states, s);
   if (r) return r;
@@ -198,7 +217,7 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
                              a.Dv, a.B, a.T, a.H, a.Dv, a.Dk, 1, 1.f, a.scale}, states, s);
   if (r || (G > 1 && (r = group_sum_launch(prec, part, a.dk, a.lddk, a, a.Dk, s)))) return r;
   r = core_launch(prec, Core{k, q, d, G > 1 ? part : a.dv, a.lddv, G > 1, a.log_decay, a.lengths, a.dsT, a.ds0, a.Dv, 1,
-                             a.B, a.T, a.H, a.Dk, a.Dv, 1, 1.f, a.scale}, states, s);
+                             a.B, a.T, a.H, a.Dk, a.Dv, 1, 1.f, a.scale}, states, s, true);
   return r || G == 1 ? r : group_sum_launch(prec, part, a.dv, a.lddv, a, a.Dv, s);
 }
 

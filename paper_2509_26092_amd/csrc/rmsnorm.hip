@@ -315,9 +315,61 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a, Dropout d)
 // The sums of dgamma of a lane's columns stay in registers over all rows of
 // the block, are joined over its row groups, and written as one partial row a
 // block: part[block][Dp] (Dp = D rounded up to 4).
+// Small calls take one launch instead: dgamma needs no row sums, so blocks of
+// their own (from row_blocks on) add up 32 columns each over all rows: 8 lanes
+// of 4 columns by 32 groups of rows, the groups' sums by fours, the fours in order.
+struct RmsParamOut {
+  float* part;      // NULL: dgamma is not wanted, or blocks of their own write it
+  int Dp, row_blocks;
+};
+template <typename T>
+__device__ inline void rms_columns(const RmsBwd& a, int c0) {
+  __shared__ float sh[32][33], sh2[8][33];
+  const int t = threadIdx.x, cl = (t & 7) * 4, rg = t >> 3, c = c0 + cl;
+  float s[4] = {};
+  if (t < 256 && c < a.D) {
+#pragma unroll 4
+    for (long r = rg; r < a.R; r += 32) {
+      const float rs = a.rstd[r];
+      const T *pd = (const T*)a.dy + r * a.lddy + c, *ph = (const T*)a.h + r * a.ldh + c;
+      T qd[4] = {}, qh[4] = {};
+      if (c + 4 <= a.D) {
+        __builtin_memcpy(qd, pd, 4 * sizeof(T));
+        __builtin_memcpy(qh, ph, 4 * sizeof(T));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (j < a.D - c) {
+            qd[j] = pd[j];
+            qh[j] = ph[j];
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += TT<T>::to_f(qd[j]) * (TT<T>::to_f(qh[j]) * rs);
+    }
+  }
+  if (t < 256)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sh[rg][cl + j] = s[j];
+  __syncthreads();
+  const int k = t & 31, q = t >> 5;
+  if (t < 256) sh2[q][k] = (sh[4 * q][k] + sh[4 * q + 1][k]) + (sh[4 * q + 2][k] + sh[4 * q + 3][k]);
+  __syncthreads();
+  if (t < 32 && c0 + k < a.D) {
+    float v = sh2[0][k];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += sh2[i][k];
+    a.dgamma[c0 + k] = v;
+  }
+}
+
 template <typename T, int L, int E, bool DROP>
-__global__ __launch_bounds__(L > 256 ? L : 256) void rms_bwd_kernel(RmsBwd a, Dropout d, float* part, int Dp) {
+__global__ __launch_bounds__(L > 256 ? L : 256) void rms_bwd_kernel(RmsBwd a, Dropout d, RmsParamOut po) {
   constexpr int VW = TT<T>::VW, NT = L > 256 ? L : 256, G = NT / L, NW = NT / 64, NV = E * VW + 1;
+  if ((int)blockIdx.x >= po.row_blocks) {
+    rms_columns<T>(a, ((int)blockIdx.x - po.row_blocks) * 32);
+    return;
+  }
   __shared__ float shp[L > 64 ? 1 : NW][L > 64 ? 1 : L * NV];
   __shared__ float sh[2][L > 64 ? L / 64 : 1][1];
   const int l = threadIdx.x % L, g = L < NT ? threadIdx.x / L : 0, D = a.D;
@@ -331,7 +383,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_bwd_kernel(RmsBwd a, Dr
 #pragma unroll
   for (int i = 0; i < NV; ++i) ag[i] = 0.f;
   const float fd = (float)D;
-  const long step = (long)gridDim.x * G;
+  const long step = (long)po.row_blocks * G;
   long r = (long)blockIdx.x * G + g;
   uint4 nd[E], nh[E], nr[E];
   T ntd, nth, ntr;
@@ -409,8 +461,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_bwd_kernel(RmsBwd a, Dr
       }
     }
   }
-  if (!part) return;
-  float* og = part + (long)blockIdx.x * Dp;
+  if (!po.part) return;
+  float* og = po.part + (long)blockIdx.x * po.Dp;
   if constexpr (L <= 64) {
     const int w = threadIdx.x >> 6, wl = threadIdx.x & 63;
 #pragma unroll
@@ -596,8 +648,10 @@ int bwd_grid(RowPath path, int L, long R, int D) {
 }
 
 template <typename T, bool DROP>
-int bwd_path(RowPath path, int L, int E, int grid, const RmsBwd& a, const Dropout& d, float* part, hipStream_t s) {
-  const int Dp = (a.D + 3) & ~3;
+int bwd_path(RowPath path, int L, int E, int grid, bool small, const RmsBwd& a, const Dropout& d, float* part,
+             hipStream_t s) {
+  const int Dp = (a.D + 3) & ~3, blocks = small ? grid + ceil_div(a.D, 32) : grid;
+  const RmsParamOut po{small ? nullptr : part, Dp, grid};
   if (path == ROW_SHORT) {
     hipLaunchKernelGGL((rms_bwd_short_kernel<T, DROP>), dim3(grid), dim3(256), 0, s, a, d, part, Dp);
     return launched();
@@ -613,7 +667,7 @@ int bwd_path(RowPath path, int L, int E, int grid, const RmsBwd& a, const Dropou
   }
 #define GO(L_, E_)                                                                                            \
   case L_ * 8 + E_:                                                                                           \
-    hipLaunchKernelGGL((rms_bwd_kernel<T, L_, E_, DROP>), dim3(grid), dim3(L_ > 256 ? L_ : 256), 0, s, a, d, part, Dp); \
+    hipLaunchKernelGGL((rms_bwd_kernel<T, L_, E_, DROP>), dim3(blocks), dim3(L_ > 256 ? L_ : 256), 0, s, a, d, po); \
     return launched();
   switch (L * 8 + E) {
     GO(1, 1) GO(2, 1) GO(4, 1) GO(8, 1) GO(16, 1) GO(32, 1) GO(64, 1) GO(64, 2) GO(256, 1) GO(256, 2) GO(512, 2)
@@ -666,20 +720,32 @@ size_t rmsnorm_bwd_workspace(int prec, long R, int D) {
   return (size_t)bwd_grid(path, L, R, D) * ((D + 3) & ~3) * 4;
 }
 
+// Calls whose dgamma blocks of their own add up, in place of a second launch that
+// joins partial sums; dy and h are read twice, from cache, and a column's sum is
+// a chain of R / 32 additions.
+static bool rms_bwd_small(int prec, long R, int D) {
+  return R <= 1024 && R * D * prec_bytes(prec) <= (8l << 20);
+}
+
 int rmsnorm_bwd_launch(int prec, const RmsBwd& a, const Dropout* d, void* ws, hipStream_t s) {
   int L = 0, E = 0, grid = 0;
+  bool small = false;
   if (a.R > 0) {
     const RowPath path = row_tile(prec, a.D, rms_max_e(prec), &L, &E);
     grid = bwd_grid(path, L, a.R, a.D);
     float* part = a.dgamma ? (float*)ws : nullptr;
+    // (dh or dx in place of dy or h would be written while the column sums read them)
+    auto apart = [&](const void* p) { return !p || (p != a.dy && p != a.h); };
+    small = part && path == ROW_TILE && apart(a.dh) && apart(a.dx) && rms_bwd_small(prec, a.R, a.D);
     const Dropout none{};
     const int r = with_prec(prec, [&](auto tag) {
       using T = decltype(tag);
-      return d ? bwd_path<T, true>(path, L, E, grid, a, *d, part, s) : bwd_path<T, false>(path, L, E, grid, a, none, part, s);
+      return d ? bwd_path<T, true>(path, L, E, grid, small, a, *d, part, s)
+               : bwd_path<T, false>(path, L, E, grid, small, a, none, part, s);
     });
     if (r) return r;
   }
-  return a.dgamma ? column_sums_launch((const float*)ws, grid, a.D, 1, a.dgamma, nullptr, s) : 0;
+  return a.dgamma && !small ? column_sums_launch((const float*)ws, grid, a.D, 1, a.dgamma, nullptr, s) : 0;
 }
 
 }  // namespace rn18
