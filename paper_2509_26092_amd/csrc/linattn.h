@@ -217,10 +217,15 @@ __device__ inline uint4 load_part(const T* p, int col, int width, bool there) {
     return q;
   }
   const bool in = there && col < width;
-  if (WIDTHS == 0) return load_chunk(in ? p : (const T*)&kNoChunk);
-  const int over = max(col + VW - width, 0);
-  const uint4 q = load_chunk(in ? p - over : (const T*)&kNoChunk);
-  const int s = 8 * (int)sizeof(T) * over & 127;
+  const int over = WIDTHS == 0 ? 0 : max(col + VW - width, 0);
+  return load_chunk(in ? p - over : (const T*)&kNoChunk);
+}
+// The part in its place, once it is there (not at the load, which it would wait
+// for).
+template <typename T, int WIDTHS>
+__device__ inline uint4 shift_part(const uint4& q, int col, int width) {
+  if (WIDTHS != 1) return q;
+  const int s = 8 * (int)sizeof(T) * max(col + TT<T>::VW - width, 0) & 127;
   const uint64_t lo = q.x | (uint64_t)q.y << 32, hi = q.z | (uint64_t)q.w << 32;
   const uint64_t l2 = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo, h2 = s >= 64 ? 0 : hi >> s;
   return make_uint4((uint32_t)l2, (uint32_t)(l2 >> 32), (uint32_t)h2, (uint32_t)(h2 >> 32));
@@ -244,7 +249,8 @@ __device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const ui
 // of them is less.
 template <typename T, int MP, int NT, int W, int WIDTHS, bool SUMS>
 __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Core c, float* seg_states,
-                                                                                           Split p, int nb_n) {
+                                                                                           Split p, int nb_n,
+                                                                                           int heads) {
   const int nseg = p.nseg, chunks = p.chunks;
   typedef Tile<T, MP, NT, W> TI;
   typedef typename OpsOf<T>::type O;
@@ -260,9 +266,14 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   L* const sV = sQ + TI::OFF_V;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i0 = lane & 15,
             g = lane >> 4;
-  // neighbours on an XCD: a head's segments, its column blocks, the heads
-  const int segs = SUMS ? nseg - 1 : nseg, id = xcd_remap(blockIdx.x, gridDim.x);
-  const int seg = id % segs, nb = id / segs % nb_n, bh = id / segs / nb_n, b = bh / c.H, h = bh - b * c.H;
+  // Blocks that share operands or lines of memory (`heads` of a token, a head's
+  // columns) go to one XCD, everything else to the XCDs in turn: neighbours along
+  // a sequence too, so that short sequences of a batch leave none of them idle.
+  const int segs = SUMS ? nseg - 1 : nseg, mates = heads * nb_n, sets = c.H / heads;
+  const int turn = blockIdx.x >> 3, mate = turn % mates, unit = turn / mates * 8 + (blockIdx.x & 7);
+  if (unit >= c.B * sets * segs) return;
+  const int seg = unit % segs, set = unit / segs % sets, b = unit / segs / sets, nb = mate / heads,
+            h = set * heads + mate % heads, bh = b * c.H + h;
   const int len = seq_len(c, b), t_first = seg * chunks * C, total = min(max(len - t_first, 0), chunks * C);
   const float g2 = c.log_decay[h] * kLog2e;
   auto pw = [&](int n) { return n <= 0 ? 1.f : __builtin_amdgcn_exp2f((float)n * g2); };
@@ -431,11 +442,11 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
     for (int s = 0; s < NQ; ++s) {
       const int at = (im + s * ROWS_M) * TI::LDM + colm;
       if (ROWS_M > C && im >= C) continue;   // (few rows for many threads)
-      if (!SUMS) put<T>(sQ + at, TI::SQ, rq[SUMS ? 0 : s]);
-      put<T>(sK + at, TI::SQ, rk[s]);
+      if (!SUMS) put<T>(sQ + at, TI::SQ, shift_part<T, WIDTHS>(rq[SUMS ? 0 : s], colm, c.M));
+      put<T>(sK + at, TI::SQ, shift_part<T, WIDTHS>(rk[s], colm, c.M));
     }
 #pragma unroll
-    for (int s = 0; s < NV; ++s) put<T>(sV + (in_ + s * ROWS_N) * TI::LDN + coln, TI::SV, rv[s]);
+    for (int s = 0; s < NV; ++s) put<T>(sV + (in_ + s * ROWS_N) * TI::LDN + coln, TI::SV, shift_part<T, WIDTHS>(rv[s], nb * TI::NB + coln, c.N));
     __syncthreads();
     if (results > 0) flush();
     if (left > C) fetch(left - C);
@@ -597,15 +608,24 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 
 template <typename T, int MP, int NT, int W, int WIDTHS>
 int chunk_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
-  const int heads = c.B * c.H, nb = ceil_div(c.N, 16 * NT * W);
+  const int nb = ceil_div(c.N, 16 * NT * W);
+  // all heads of a token together where there are enough units to deal out so,
+  // otherwise those that share keys and values. (256x196 tokens, 8 heads of 64,
+  // bf16 forward: 66 us, every head for itself 70; ragged sequences in 16
+  // segments, fp16 backward: 333 us, one contiguous range of blocks an XCD 450.)
+  auto heads = [&](int segs) { return (long)c.B * segs >= 64 ? c.H : std::max(c.q.group, c.k.group); };
+  auto grid = [&](int segs) {
+    const int h = heads(segs);
+    return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb);
+  };
   if (p.nseg > 1 && !p.there) {
-    hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), dim3(heads * nb * (p.nseg - 1)), dim3(64 * W), 0,
-                       s, c, states, p, nb);
+    hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), grid(p.nseg - 1), dim3(64 * W), 0, s, c, states,
+                       p, nb, heads(p.nseg - 1));
     const int r = segments_launch(c, states, p, s);
     if (r) return r;
   }
-  hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), dim3(heads * nb * p.nseg), dim3(64 * W), 0, s, c,
-                     states, p, nb);
+  hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), grid(p.nseg), dim3(64 * W), 0, s, c, states, p,
+                     nb, heads(p.nseg));
   return launched();
 }
 
