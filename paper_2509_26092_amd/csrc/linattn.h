@@ -34,19 +34,37 @@ struct Core {
   int s_m, s_n;
   int B, T, H, M, N, rev;
   float out_scale, kv_scale;
+  float* states;   // of segments, element (m, n) at m * st_m + n * st_n
+  int st_m, st_n;
+};
+// Passes of one launch, which share their sizes' class (see shape_of): `n` of
+// them, whose first `sums` leave the states that a segment starts from.
+constexpr int kPasses = 3;
+struct Cores {
+  Core c[kPasses];
+  int n, sums;
 };
 
 // A call's split: segments of a sequence, chunks of a segment.
 struct Split {
   int nseg, chunks;
-  int s_m, s_n;   // element (m, n) of a segment's state
-  bool there;     // another pass has left the segments' states already
 };
+// A pass's kernel: rows of the state, waves of a block (32 columns each; eight
+// waves of 256 rows would not fit in the registers), and WIDTHS (below).
+struct Shape {
+  int rows, waves, widths;
+  bool operator==(const Shape& o) const { return rows == o.rows && waves == o.waves && widths == o.widths; }
+};
+inline Shape shape_of(int prec, const Core& c) {
+  const int vw = prec_vw(prec), rows = c.M <= 64 ? 64 : c.M <= 128 ? 128 : 256;
+  return Shape{rows, c.N <= 64 ? 2 : c.N <= 128 || rows == 256 ? 4 : 8,
+               std::min(c.M, c.N) < vw ? 2 : c.M % vw || c.N % vw ? 1 : 0};
+}
 // What the segments before each one leave of the state, in place of their sums.
-int segments_launch(const Core& c, float* states, const Split& p, hipStream_t s);
-int chunks_launch_fp32(const Core& c, const Split& p, float* states, hipStream_t s);
-int chunks_launch_bf16(const Core& c, const Split& p, float* states, hipStream_t s);
-int chunks_launch_fp16(const Core& c, const Split& p, float* states, hipStream_t s);
+int segments_launch(const Cores& cs, const Split& p, hipStream_t s);
+int chunks_launch_fp32(const Cores& cs, const Split& p, hipStream_t s);
+int chunks_launch_bf16(const Cores& cs, const Split& p, hipStream_t s);
+int chunks_launch_fp16(const Cores& cs, const Split& p, hipStream_t s);
 
 namespace {
 
@@ -248,9 +266,10 @@ __device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const ui
 // WIDTHS 0: M and N are whole chunks of 16 bytes, 1: a chunk at least each, 2: one
 // of them is less.
 template <typename T, int MP, int NT, int W, int WIDTHS, bool SUMS>
-__global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Core c, float* seg_states,
-                                                                                           Split p, int nb_n,
+__global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Cores cs, Split p, int nb_n,
                                                                                            int heads) {
+  const Core c = cs.c[blockIdx.y];
+  float* const seg_states = c.states;
   const int nseg = p.nseg, chunks = p.chunks;
   typedef Tile<T, MP, NT, W> TI;
   typedef typename OpsOf<T>::type O;
@@ -288,7 +307,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   {
     const bool stored = !SUMS && nseg > 1;
     const float* src = stored ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_in + (long)bh * c.M * c.N;
-    const int s_m = stored ? p.s_m : c.s_m, s_n = stored ? p.s_n : c.s_n;
+    const int s_m = stored ? c.st_m : c.s_m, s_n = stored ? c.st_n : c.s_n;
     const bool any = !SUMS && (stored || c.s_in);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -592,7 +611,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 
   if (!works || (!SUMS && (!c.s_out || seg != nseg - 1))) return;
   float* to = SUMS ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_out + (long)bh * c.M * c.N;
-  const int s_m = SUMS ? p.s_m : c.s_m, s_n = SUMS ? p.s_n : c.s_n;
+  const int s_m = SUMS ? c.st_m : c.s_m, s_n = SUMS ? c.st_n : c.s_n;
   int m0 = 4 * g;   // (where elements lie is found again, not kept from the start)
   asm volatile("" : "+v"(m0));
 #pragma unroll
@@ -607,25 +626,28 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 }
 
 template <typename T, int MP, int NT, int W, int WIDTHS>
-int chunk_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
+int chunk_launch(const Cores& cs, const Split& p, hipStream_t s) {
+  const Core& c = cs.c[0];
   const int nb = ceil_div(c.N, 16 * NT * W);
   // all heads of a token together where there are enough units to deal out so,
   // otherwise those that share keys and values. (256x196 tokens, 8 heads of 64,
   // bf16 forward: 66 us, every head for itself 70; ragged sequences in 16
   // segments, fp16 backward: 333 us, one contiguous range of blocks an XCD 450.)
-  auto heads = [&](int segs) { return (long)c.B * segs >= 64 ? c.H : std::max(c.q.group, c.k.group); };
-  auto grid = [&](int segs) {
+  int mates = 1;
+  for (int i = 0; i < cs.n; ++i) mates = std::max({mates, cs.c[i].q.group, cs.c[i].k.group});
+  auto heads = [&](int segs) { return (long)c.B * segs >= 64 ? c.H : mates; };
+  auto grid = [&](int segs, int passes) {
     const int h = heads(segs);
-    return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb);
+    return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb, passes);
   };
-  if (p.nseg > 1 && !p.there) {
-    hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), grid(p.nseg - 1), dim3(64 * W), 0, s, c, states,
-                       p, nb, heads(p.nseg - 1));
-    const int r = segments_launch(c, states, p, s);
+  if (p.nseg > 1 && cs.sums) {
+    hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), grid(p.nseg - 1, cs.sums), dim3(64 * W), 0, s,
+                       cs, p, nb, heads(p.nseg - 1));
+    const int r = segments_launch(cs, p, s);
     if (r) return r;
   }
-  hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), grid(p.nseg), dim3(64 * W), 0, s, c, states, p,
-                     nb, heads(p.nseg));
+  hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, false>), grid(p.nseg, cs.n), dim3(64 * W), 0, s, cs, p, nb,
+                     heads(p.nseg));
   return launched();
 }
 
@@ -634,27 +656,28 @@ int chunk_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
 // 128: too few waves beside the vector units' work on X), and 16 too (90, 658:
 // every wave computes the scores).
 template <typename T, int WIDTHS>
-int widths_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
-  auto waves = [&](auto rows) {
-    constexpr int MP = decltype(rows)::value;
-    // (for widths below a chunk of 16 bytes, M or N is small)
-    if (c.N <= 64) return chunk_launch<T, MP, 2, 2, WIDTHS>(c, p, states, s);
-    if constexpr (WIDTHS < 2 || MP == 64)
-      // (eight waves of 256 rows would not fit in the registers)
-      return c.N <= 128 || MP > 128 ? chunk_launch<T, MP, 2, 4, WIDTHS>(c, p, states, s)
-                                    : chunk_launch<T, MP, 2, (MP > 128 ? 4 : 8), WIDTHS>(c, p, states, s);
+int widths_launch(const Cores& cs, int rows, int waves, const Split& p, hipStream_t s) {
+  auto go = [&](auto r) {
+    constexpr int MP = decltype(r)::value;
+    if (waves == 2) return chunk_launch<T, MP, 2, 2, WIDTHS>(cs, p, s);
+    // (widths below a chunk of 16 bytes are M's or N's, so that not both are large)
+    if constexpr (WIDTHS < 2 || MP == 64) {
+      if (waves == 4) return chunk_launch<T, MP, 2, 4, WIDTHS>(cs, p, s);
+      if constexpr (MP <= 128) return chunk_launch<T, MP, 2, 8, WIDTHS>(cs, p, s);
+    }
     return -1;
   };
-  if (c.M <= 64) return waves(std::integral_constant<int, 64>());
-  if (c.M <= 128) return waves(std::integral_constant<int, 128>());
-  return waves(std::integral_constant<int, 256>());
+  if (rows == 64) return go(std::integral_constant<int, 64>());
+  if (rows == 128) return go(std::integral_constant<int, 128>());
+  return go(std::integral_constant<int, 256>());
 }
 
 template <typename T>
-int chunks_launch(const Core& c, const Split& p, float* states, hipStream_t s) {
-  constexpr int VW = TT<T>::VW;
-  if (c.M < VW || c.N < VW) return widths_launch<T, 2>(c, p, states, s);
-  return c.M % VW || c.N % VW ? widths_launch<T, 1>(c, p, states, s) : widths_launch<T, 0>(c, p, states, s);
+int chunks_launch(const Cores& cs, const Split& p, hipStream_t s) {
+  const Shape h = shape_of(prec_of<T>(), cs.c[0]);
+  if (h.widths == 0) return widths_launch<T, 0>(cs, h.rows, h.waves, p, s);
+  if (h.widths == 1) return widths_launch<T, 1>(cs, h.rows, h.waves, p, s);
+  return widths_launch<T, 2>(cs, h.rows, h.waves, p, s);
 }
 
 }  // namespace

@@ -16,7 +16,8 @@ namespace {
 // launch leaves what each segment (but the last) adds to the state, this one
 // turns these sums into the states that the segments start from, element by
 // element in order, and a last one takes the segments from there.
-__global__ __launch_bounds__(256) void linattn_segments_kernel(Core c, float* seg_states, Split p, int tokens) {
+__global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p, int tokens) {
+  const Core c = cs.c[blockIdx.z];
   constexpr int U = 8;   // sums loaded at a time
   const int per = c.M * c.N, e = blockIdx.x * 256 + threadIdx.x, bh = blockIdx.y, b = bh / c.H;
   if (e >= per) return;
@@ -24,7 +25,7 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Core c, float* se
   const float g = c.log_decay[bh - b * c.H];
   float x = c.s_in ? c.s_in[(long)bh * per + (long)m * c.s_m + (long)n * c.s_n] : 0.f;
   const float whole = expm1f((float)tokens * g);
-  float* at = seg_states + (long)bh * p.nseg * per + (long)m * p.s_m + (long)n * p.s_n;
+  float* at = c.states + (long)bh * p.nseg * per + (long)m * c.st_m + (long)n * c.st_n;
   for (int s = 0; s < p.nseg; s += U) {
     float add[U];
 #pragma unroll
@@ -41,21 +42,27 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Core c, float* se
 }
 
 // The gradients of query heads that share a key head, added up in the order
-// of the heads: part fp32 [tokens][H][N] to out [tokens][H / group][N].
+// of the heads: part fp32 [tokens][H][N] to out [tokens][H / group][N]; dk and dv
+// in one launch.
+struct GroupSum {
+  const float* part[2];
+  void* out[2];
+  long ldo[2];
+  int N[2];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void linattn_group_sum_kernel(const float* __restrict__ part, T* out, long ldo,
-                                                                const int32_t* lengths, int B, int T_, int H, int group,
-                                                                int N) {
-  const int Hk = H / group, cols = Hk * N;
+__global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, const int32_t* lengths, int B, int T_, int H,
+                                                                int group) {
+  const int w = blockIdx.y, N = a.N[w], Hk = H / group, cols = Hk * N;
   const long total = (long)B * T_ * cols;
   for (long i = blockIdx.x * 256l + threadIdx.x; i < total; i += gridDim.x * 256l) {
     const long row = i / cols;
     const int col = (int)(i - row * cols), hk = col / N, n = col - hk * N;
     if (lengths && (int)(row % T_) >= lengths[row / T_]) continue;
-    const float* p = part + (row * H + (long)hk * group) * N + n;
+    const float* p = a.part[w] + (row * H + (long)hk * group) * N + n;
     float s = p[0];
     for (int g = 1; g < group; ++g) s += p[(long)g * N];
-    out[row * ldo + col] = TT<T>::from_f(s);
+    ((T*)a.out[w])[row * a.ldo[w] + col] = TT<T>::from_f(s);
   }
 }
 
@@ -129,46 +136,30 @@ Split split_of(int B, int T, int H, int M, int N) {
   const long units = std::max(1l, (long)B * H * ceil_div(std::max(M, N), 64)), want = (all <= 256 ? 8l : 4l) * plan_cus();
   const long nseg = std::max(1l, units >= 2l * plan_cus() ? 1 : std::min((want + units - 1) / units, (long)all / 8));
   const int chunks = ceil_div(all, nseg);
-  return Split{ceil_div(all, chunks), chunks, N, 1, false};
+  return Split{ceil_div(all, chunks), chunks};
 }
 size_t split_bytes(int B, int T, int H, int M, int N) {
   const Split p = split_of(B, T, H, M, N);
   return p.nseg > 1 ? (size_t)B * H * p.nseg * M * N * 4 : 0;
 }
 
-// `states`: split_bytes of the pass; `there`: the pass before, on the state's
-// transpose, has left its segments' states in them.
-int core_launch(int prec, const Core& c, float* states, hipStream_t s, bool there = false) {
+int cores_launch(int prec, const Cores& cs, hipStream_t s) {
+  const Core& c = cs.c[0];
   if (c.B <= 0) return 0;
-  Split p = split_of(c.B, c.T, c.H, c.M, c.N);
-  if (there) {
-    p.s_m = 1;
-    p.s_n = c.M;
-    p.there = true;
-  }
+  const Split p = split_of(c.B, c.T, c.H, c.M, c.N);
   switch (prec) {
-    case PREC_F32: return chunks_launch_fp32(c, p, states, s);
-    case PREC_BF16: return chunks_launch_bf16(c, p, states, s);
-    case PREC_F16: return chunks_launch_fp16(c, p, states, s);
+    case PREC_F32: return chunks_launch_fp32(cs, p, s);
+    case PREC_BF16: return chunks_launch_bf16(cs, p, s);
+    case PREC_F16: return chunks_launch_fp16(cs, p, s);
     default: return -1;
   }
 }
 
-int group_sum_launch(int prec, const float* part, void* out, long ldo, const LinattnBwd& a, int N, hipStream_t s) {
-  const long total = (long)a.B * a.T * a.Hk * N;
-  if (total <= 0) return 0;
-  return with_prec(prec, [&](auto tag) {
-    using T = decltype(tag);
-    hipLaunchKernelGGL(linattn_group_sum_kernel<T>, dim3(even_grid((total + 255) / 256, 16)), dim3(256), 0, s, part,
-                       (T*)out, ldo, a.lengths, a.B, a.T, a.H, a.H / a.Hk, N);
-    return launched();
-  });
-}
-
 }  // namespace
 
-int segments_launch(const Core& c, float* states, const Split& p, hipStream_t s) {
-  hipLaunchKernelGGL(linattn_segments_kernel, dim3(ceil_div((long)c.M * c.N, 256), c.B * c.H), dim3(256), 0, s, c, states,
+int segments_launch(const Cores& cs, const Split& p, hipStream_t s) {
+  const Core& c = cs.c[0];
+  hipLaunchKernelGGL(linattn_segments_kernel, dim3(ceil_div((long)c.M * c.N, 256), c.B * c.H, cs.sums), dim3(256), 0, s, cs,
                      p, p.chunks * kChunk);
   return launched();
 }
@@ -179,8 +170,11 @@ size_t linattn_fwd_workspace(int, int B, int T, int H, int, int Dk, int Dv) {
 
 int linattn_fwd_launch(int prec, const LinattnFwd& a, void* ws, hipStream_t s) {
   const int G = a.H / a.Hk;
-  return core_launch(prec, Core{{a.q, a.ldq, 1}, {a.k, a.ldk, G}, {a.v, a.ldv, G}, a.o, a.ldo, 0, a.log_decay, a.lengths,
-                                a.s0, a.sT, a.Dv, 1, a.B, a.T, a.H, a.Dk, a.Dv, 0, a.scale, 1.f}, (float*)ws, s);
+  Cores cs{};
+  cs.c[0] = Core{{a.q, a.ldq, 1}, {a.k, a.ldk, G}, {a.v, a.ldv, G}, a.o, a.ldo, 0, a.log_decay, a.lengths, a.s0, a.sT,
+                 a.Dv, 1, a.B, a.T, a.H, a.Dk, a.Dv, 0, a.scale, 1.f, (float*)ws, a.Dv, 1};
+  cs.n = cs.sums = 1;
+  return cores_launch(prec, cs, s);
 }
 
 int linattn_step_launch(int prec, const LinattnFwd& a, hipStream_t s) {
@@ -194,31 +188,46 @@ int linattn_step_launch(int prec, const LinattnFwd& a, hipStream_t s) {
   });
 }
 
-// Query heads' own gradients of shared keys or values, then a pass's segment
-// states.
-static size_t group_bytes(int B, int T, int H, int Hk, int Dk, int Dv) {
-  return H > Hk ? (((size_t)B * T * H * std::max(Dk, Dv) * 4 + 255) & ~(size_t)255) : 0;
+// Query heads' own gradients of shared keys and values, then the segment states
+// of the forward and the reverse passes.
+static size_t group_bytes(int B, int T, int H, int Hk, int D) {
+  return H > Hk ? (((size_t)B * T * H * D * 4 + 255) & ~(size_t)255) : 0;
 }
 size_t linattn_bwd_workspace(int, int B, int T, int H, int Hk, int Dk, int Dv) {
-  return group_bytes(B, T, H, Hk, Dk, Dv) +
-         std::max(split_bytes(B, T, H, Dv, Dk), split_bytes(B, T, H, Dk, Dv));
+  return group_bytes(B, T, H, Hk, Dk) + group_bytes(B, T, H, Hk, Dv) + 2 * split_bytes(B, T, H, Dk, Dv);
 }
 
 int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   const int G = a.H / a.Hk;
-  float *part = (float*)ws, *states = (float*)((char*)ws + group_bytes(a.B, a.T, a.H, a.Hk, a.Dk, a.Dv));
+  char* at = (char*)ws;
+  float* pk = (float*)at;
+  at += group_bytes(a.B, a.T, a.H, a.Hk, a.Dk);
+  float* pv = (float*)at;
+  at += group_bytes(a.B, a.T, a.H, a.Hk, a.Dv);
+  float *sf = (float*)at, *sr = (float*)(at + split_bytes(a.B, a.T, a.H, a.Dk, a.Dv));
   const Operand q{a.q, a.ldq, 1}, k{a.k, a.ldk, G}, v{a.v, a.ldv, G}, d{a.dout, a.lddout, 1};
   // dq and dk: on the state's transpose, whose elements are taken the other way
-  // round; dv goes with dk's segments
-  int r = core_launch(prec, Core{d, v, k, a.dq, a.lddq, 0, a.log_decay, a.lengths, a.s0, nullptr, 1, a.Dv, a.B, a.T,
-                                 a.H, a.Dv, a.Dk, 0, a.scale, 1.f}, states, s);
-  if (r) return r;
-  r = core_launch(prec, Core{v, d, q, G > 1 ? part : a.dk, a.lddk, G > 1, a.log_decay, a.lengths, a.dsT, nullptr, 1,
-                             a.Dv, a.B, a.T, a.H, a.Dv, a.Dk, 1, 1.f, a.scale}, states, s);
-  if (r || (G > 1 && (r = group_sum_launch(prec, part, a.dk, a.lddk, a, a.Dk, s)))) return r;
-  r = core_launch(prec, Core{k, q, d, G > 1 ? part : a.dv, a.lddv, G > 1, a.log_decay, a.lengths, a.dsT, a.ds0, a.Dv, 1,
-                             a.B, a.T, a.H, a.Dk, a.Dv, 1, 1.f, a.scale}, states, s, true);
-  return r || G == 1 ? r : group_sum_launch(prec, part, a.dv, a.lddv, a, a.Dv, s);
+  // round; dv goes with dk's segments. All in one launch where their kernel is
+  // the same: none waits for the last blocks of another, and what they share is
+  // read together.
+  const Core dq{d, v, k, a.dq, a.lddq, 0, a.log_decay, a.lengths, a.s0, nullptr, 1, a.Dv, a.B, a.T, a.H, a.Dv, a.Dk, 0,
+                a.scale, 1.f, sf, a.Dk, 1};
+  const Core dk{v, d, q, G > 1 ? pk : a.dk, a.lddk, G > 1, a.log_decay, a.lengths, a.dsT, nullptr, 1, a.Dv, a.B, a.T, a.H,
+                a.Dv, a.Dk, 1, 1.f, a.scale, sr, a.Dk, 1};
+  const Core dv{k, q, d, G > 1 ? pv : a.dv, a.lddv, G > 1, a.log_decay, a.lengths, a.dsT, a.ds0, a.Dv, 1, a.B, a.T, a.H,
+                a.Dk, a.Dv, 1, 1.f, a.scale, sr, 1, a.Dk};
+  const bool one = shape_of(prec, dq) == shape_of(prec, dv) && !(a.ds0 && a.ds0 == a.dsT);   // (dk reads dsT too)
+  int r = cores_launch(prec, one ? Cores{{dq, dk, dv}, 3, 2} : Cores{{dq, dk, dk}, 2, 2}, s);
+  if (!r && !one) r = cores_launch(prec, Cores{{dv, dv, dv}, 1, 0}, s);
+  const long most = (long)a.B * a.T * a.Hk * std::max(a.Dk, a.Dv);
+  if (r || G == 1 || most <= 0) return r;
+  const GroupSum gs{{pk, pv}, {a.dk, a.dv}, {a.lddk, a.lddv}, {a.Dk, a.Dv}};
+  return with_prec(prec, [&](auto tag) {
+    using T = decltype(tag);
+    hipLaunchKernelGGL(linattn_group_sum_kernel<T>, dim3(even_grid((most + 255) / 256, 8), 2), dim3(256), 0, s, gs,
+                       a.lengths, a.B, a.T, a.H, G);
+    return launched();
+  });
 }
 
 }  // namespace rn18

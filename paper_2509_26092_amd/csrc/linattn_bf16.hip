@@ -3,8 +3,6 @@
 
 namespace rn18 {
 
-int chunks_launch_bf16(const Core& c, const Split& p, float* states, hipStream_t s) {
-  return chunks_launch<bf16_t>(c, p, states, s);
-}
+int chunks_launch_bf16(const Cores& cs, const Split& p, hipStream_t s) { return chunks_launch<bf16_t>(cs, p, s); }
 
 }  // namespace rn18

@@ -3,8 +3,6 @@
 
 namespace rn18 {
 
-int chunks_launch_fp32(const Core& c, const Split& p, float* states, hipStream_t s) {
-  return chunks_launch<float>(c, p, states, s);
-}
+int chunks_launch_fp32(const Cores& cs, const Split& p, hipStream_t s) { return chunks_launch<float>(cs, p, s); }
 
 }  // namespace rn18
