@@ -268,8 +268,6 @@ __device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const ui
 template <typename T, int MP, int NT, int W, int WIDTHS, bool SUMS>
 __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_chunk_kernel(Cores cs, Split p, int nb_n,
                                                                                            int heads) {
-  const Core c = cs.c[blockIdx.y];
-  float* const seg_states = c.states;
   const int nseg = p.nseg, chunks = p.chunks;
   typedef Tile<T, MP, NT, W> TI;
   typedef typename OpsOf<T>::type O;
@@ -286,13 +284,17 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, i0 = lane & 15,
             g = lane >> 4;
   // Blocks that share operands or lines of memory (`heads` of a token, a head's
-  // columns) go to one XCD, everything else to the XCDs in turn: neighbours along
-  // a sequence too, so that short sequences of a batch leave none of them idle.
-  const int segs = SUMS ? nseg - 1 : nseg, mates = heads * nb_n, sets = c.H / heads;
+  // columns, the launch's passes) go to one XCD next to each other, everything
+  // else to the XCDs in turn: neighbours along a sequence too, so that short
+  // sequences of a batch leave none of them idle.
+  const int passes = SUMS ? cs.sums : cs.n, segs = SUMS ? p.nseg - 1 : p.nseg, mates = heads * nb_n * passes;
   const int turn = blockIdx.x >> 3, mate = turn % mates, unit = turn / mates * 8 + (blockIdx.x & 7);
+  const Core c = cs.c[mate % passes];
+  const int sets = c.H / heads;
   if (unit >= c.B * sets * segs) return;
-  const int seg = unit % segs, set = unit / segs % sets, b = unit / segs / sets, nb = mate / heads,
-            h = set * heads + mate % heads, bh = b * c.H + h;
+  const int seg = unit % segs, set = unit / segs % sets, b = unit / segs / sets, nb = mate / passes % nb_n,
+            h = set * heads + mate / passes / nb_n, bh = b * c.H + h;
+  float* const seg_states = c.states;
   const int len = seq_len(c, b), t_first = seg * chunks * C, total = min(max(len - t_first, 0), chunks * C);
   const float g2 = c.log_decay[h] * kLog2e;
   auto pw = [&](int n) { return n <= 0 ? 1.f : __builtin_amdgcn_exp2f((float)n * g2); };
@@ -638,7 +640,7 @@ int chunk_launch(const Cores& cs, const Split& p, hipStream_t s) {
   auto heads = [&](int segs) { return (long)c.B * segs >= 64 ? c.H : mates; };
   auto grid = [&](int segs, int passes) {
     const int h = heads(segs);
-    return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb, passes);
+    return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb * passes);
   };
   if (p.nseg > 1 && cs.sums) {
     hipLaunchKernelGGL((linattn_chunk_kernel<T, MP, NT, W, WIDTHS, true>), grid(p.nseg - 1, cs.sums), dim3(64 * W), 0, s,
