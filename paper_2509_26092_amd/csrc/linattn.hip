@@ -50,20 +50,32 @@ struct GroupSum {
   long ldo[2];
   int N[2];
 };
-template <typename T>
+// V columns a thread, tiles of 16 rows a block.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, const int32_t* lengths, int B, int T_, int H,
                                                                 int group) {
-  const int w = blockIdx.y, N = a.N[w], Hk = H / group, cols = Hk * N;
-  const long total = (long)B * T_ * cols;
-  for (long i = blockIdx.x * 256l + threadIdx.x; i < total; i += gridDim.x * 256l) {
-    const long row = i / cols;
-    const int col = (int)(i - row * cols), hk = col / N, n = col - hk * N;
-    if (lengths && (int)(row % T_) >= lengths[row / T_]) continue;
-    const float* p = a.part[w] + (row * H + (long)hk * group) * N + n;
-    float s = p[0];
-    for (int g = 1; g < group; ++g) s += p[(long)g * N];
-    ((T*)a.out[w])[row * a.ldo[w] + col] = TT<T>::from_f(s);
-  }
+  const int w = blockIdx.y, N = a.N[w], Hk = H / group, units = Hk * N / V;
+  const long rows = (long)B * T_;
+  for (long r0 = blockIdx.x * 16l; r0 < rows; r0 += gridDim.x * 16l)
+    for (int e = threadIdx.x; e < 16 * units; e += 256) {
+      const long row = r0 + e / units;
+      if (row >= rows || (lengths && (int)(row % T_) >= lengths[row / T_])) continue;
+      const int col = e % units * V, hk = col / N;
+      const float* p = a.part[w] + (row * H + (long)hk * group) * N + (col - hk * N);
+      float s[V];
+      __builtin_memcpy(s, p, sizeof(s));
+#pragma unroll 4
+      for (int g = 1; g < group; ++g) {
+        float t[V];
+        __builtin_memcpy(t, p + (long)g * N, sizeof(t));
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] += t[j];
+      }
+      T o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = TT<T>::from_f(s[j]);
+      __builtin_memcpy((T*)a.out[w] + row * a.ldo[w] + col, o, sizeof(o));
+    }
 }
 
 // One token: a block per sequence and head, a lane per four columns of the
@@ -219,13 +231,16 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   const bool one = shape_of(prec, dq) == shape_of(prec, dv) && !(a.ds0 && a.ds0 == a.dsT);   // (dk reads dsT too)
   int r = cores_launch(prec, one ? Cores{{dq, dk, dv}, 3, 2} : Cores{{dq, dk, dk}, 2, 2}, s);
   if (!r && !one) r = cores_launch(prec, Cores{{dv, dv, dv}, 1, 0}, s);
-  const long most = (long)a.B * a.T * a.Hk * std::max(a.Dk, a.Dv);
-  if (r || G == 1 || most <= 0) return r;
+  const long rows = (long)a.B * a.T;
+  if (r || G == 1 || rows <= 0) return r;
   const GroupSum gs{{pk, pv}, {a.dk, a.dv}, {a.lddk, a.lddv}, {a.Dk, a.Dv}};
+  const dim3 grid((unsigned)std::min((rows + 15) / 16, 32768l), 2);
   return with_prec(prec, [&](auto tag) {
     using T = decltype(tag);
-    hipLaunchKernelGGL(linattn_group_sum_kernel<T>, dim3(even_grid((most + 255) / 256, 8), 2), dim3(256), 0, s, gs,
-                       a.lengths, a.B, a.T, a.H, G);
+    if (a.Dk % 4 == 0 && a.Dv % 4 == 0)
+      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 4>), grid, dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
+    else
+      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 1>), grid, dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
     return launched();
   });
 }
