@@ -113,11 +113,18 @@ template <int P> struct Ops16 {
       for (int j = B - 1; j >= 0; --j)
         if (i + j < LIM) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8(a.p[i]), v8(b.p[j]), acc, 0, 0, 0);
   }
-  // The leading parts of two values, which keep the rest.
+  // The leading parts of two values, which keep the rest (exact: one product
+  // with -1 and one with 0 each, in place of a shift or mask and a difference;
+  // what is not finite reaches its neighbour, which is of the same sum always).
+  // The factors go through registers: as literals, {-1, 0} was encoded as an
+  // inline constant that the unit reads as {0, -1}.
   __device__ static inline uint32_t take(float& a, float& b) {
+    uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+    asm("" : "+s"(first), "+s"(second));
     const uint32_t h = f2bf2(a, b);
-    a -= __builtin_bit_cast(float, h << 16);
-    b -= __builtin_bit_cast(float, h & 0xffff0000u);
+    const bf16x2_t p = __builtin_bit_cast(bf16x2_t, h);
+    a = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, first), a, false);
+    b = __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, second), b, false);
     return h;
   }
   template <int N>
@@ -306,11 +313,13 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   auto col_of = [](int nt, int x) { return 32 * (nt / 2) + 8 * (x >> 2) + 4 * (nt & 1) + (x & 3); };
 
   floatx4_t X[MT][NT];   // rows 16 mt + 4 g + r, column col_of(nt, i0)
+  bool empty;            // X is zero
   {
     const bool stored = !SUMS && nseg > 1;
     const float* src = stored ? seg_states + ((long)bh * nseg + seg) * c.M * c.N : c.s_in + (long)bh * c.M * c.N;
     const int s_m = stored ? c.st_m : c.s_m, s_n = stored ? c.st_n : c.s_n;
     const bool any = !SUMS && (stored || c.s_in);
+    empty = !any;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -455,6 +464,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
     po += C * so;
   };
 
+  const bool last_state = SUMS || (c.s_out && seg == nseg - 1);   // the state behind the last chunk is wanted
   if (total > 0) fetch(total);
   for (int left = total; left > 0; left -= C) {
     if (left < C) tails(left);
@@ -494,6 +504,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 #pragma unroll
           for (int it = jt; it < CT; ++it) O::template mma<2>(P[it][jt], k, q[it]);
         }
+        if (empty) continue;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float x[O::EV];
@@ -515,47 +526,50 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
         for (int nt = 0; nt < NT; ++nt) out[it][nt] *= up[it];
       }
     }
+    empty = false;
 
-    // the state behind the chunk
     typename O::In V[C / KB][NT];
     float bad = 0.f;   // NaN if one of the chunk's v is not finite
 #pragma unroll
     for (int jb = 0; jb < C / KB; ++jb)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        V[jb][nt] = frag_col(sV, TI::LDN, TI::SV, jb * KB, w * 16 * NT + col_of(nt, 0), 8);
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) X[mt][nt][r] = fmaf(X[mt][nt][r], less, X[mt][nt][r]);
-#pragma unroll
-    for (int jb = 0; jb < C / KB; ++jb) {
-      typename O::In K[MT > 4 ? 1 : MT];   // few rows: their operands once for all columns, otherwise the other way round
-      typename O::Three D[MT > 4 ? NT : 1];
-      if (MT <= 4)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) K[MT > 4 ? 0 : mt] = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
-#pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float v[O::EV];
-        O::values(V[jb][nt], v);
+        V[jb][nt] = frag_col(sV, TI::LDN, TI::SV, jb * KB, w * 16 * NT + col_of(nt, 0), 8);
+        if (!SUMS) bad = O::not_finite(V[jb][nt], bad);
+      }
+    if (left > C || last_state) {   // the state behind the chunk
 #pragma unroll
-        for (int e = 0; e < O::EV; ++e) v[e] *= tail[jb][e];
-        bad = O::not_finite(V[jb][nt], bad);
-        D[MT > 4 ? nt : 0] = O::template parts<3>(v);
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) X[mt][nt][r] = fmaf(X[mt][nt][r], less, X[mt][nt][r]);
+#pragma unroll
+      for (int jb = 0; jb < C / KB; ++jb) {
+        typename O::In K[MT > 4 ? 1 : MT];   // few rows: their operands once for all columns, otherwise the other way round
+        typename O::Three D[MT > 4 ? NT : 1];
         if (MT <= 4)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) O::template mma<3>(X[mt][nt], K[MT > 4 ? 0 : mt], D[0]);
-      }
-      if (MT > 4)
+          for (int mt = 0; mt < MT; ++mt) K[MT > 4 ? 0 : mt] = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const auto k = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
+        for (int nt = 0; nt < NT; ++nt) {
+          float v[O::EV];
+          O::values(V[jb][nt], v);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) O::template mma<3>(X[mt][nt], k, D[MT > 4 ? nt : 0]);
+          for (int e = 0; e < O::EV; ++e) v[e] *= tail[jb][e];
+          D[MT > 4 ? nt : 0] = O::template parts<3>(v);
+          if (MT <= 4)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) O::template mma<3>(X[mt][nt], K[MT > 4 ? 0 : mt], D[0]);
         }
+        if (MT > 4)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const auto k = frag_col(sK, TI::LDM, TI::SQ, jb * KB, 16 * mt, 4);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O::template mma<3>(X[mt][nt], k, D[MT > 4 ? nt : 0]);
+          }
+      }
     }
 
     if constexpr (!SUMS) {
