@@ -68,6 +68,20 @@ int chunks_launch_fp16(const Cores& cs, const Split& p, hipStream_t s);
 
 namespace {
 
+// What n tokens leave of a state, decay^n of it: as x + (decay^n - 1) x where most
+// of it stays, since the factor's rounding would add up over many such steps, and
+// as decay^n x where little does, which the difference would round away.
+struct Kept {
+  float factor;
+  bool by_rest;
+  __device__ inline float operator()(float x) const { return fmaf(x, factor, by_rest ? x : 0.f); }
+};
+__device__ inline Kept kept(int n, float g) {
+  const float t = n > 0 ? (float)n * g : 0.f;
+  const bool by_rest = t > -0.69f;
+  return Kept{by_rest ? expm1f(t) : expf(t), by_rest};
+}
+
 // Tokens of sequence b.
 __device__ inline int seq_len(const Core& c, int b) {
   return c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
@@ -398,7 +412,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   // and in the one below, of a token's place, and of what is left of a chunk
   // behind a token (anew for a partial last chunk)
   const float scale = c.kv_scale * c.out_scale;
-  float diag[4], below[4], up[CT], tail[C / KB][O::EV], less;
+  float diag[4], below[4], up[CT], tail[C / KB][O::EV];
+  Kept less{};
   if (!SUMS) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -414,7 +429,7 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 #pragma unroll
       for (int e = 0; e < O::EV; ++e)
         tail[jb][e] = pw(n - 1 + c.rev - (jb * KB + 16 * (e >> 2) + 4 * g + (e & 3))) * c.kv_scale;
-    less = expm1f((float)n * c.log_decay[h]);   // decay^n - 1: exact near 1, where many chunks multiply
+    less = kept(n, c.log_decay[h]);
   };
   tails(C);
   const int col_out = n_wave + 8 * g;
@@ -538,12 +553,18 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
         if (!SUMS) bad = O::not_finite(V[jb][nt], bad);
       }
     if (left > C || last_state) {   // the state behind the chunk
+      if (!less.by_rest)   // (then the sum below leaves X as it is)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) X[mt][nt] *= less.factor;
+      const float rest = less.by_rest ? less.factor : 0.f;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) X[mt][nt][r] = fmaf(X[mt][nt][r], less, X[mt][nt][r]);
+          for (int r = 0; r < 4; ++r) X[mt][nt][r] = fmaf(X[mt][nt][r], rest, X[mt][nt][r]);
 #pragma unroll
       for (int jb = 0; jb < C / KB; ++jb) {
         typename O::In K[MT > 4 ? 1 : MT];   // few rows: their operands once for all columns, otherwise the other way round

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p
   const int len = seq_len(c, b), m = e / c.N, n = e - m * c.N;
   const float g = c.log_decay[bh - b * c.H];
   float x = c.s_in ? c.s_in[(long)bh * per + (long)m * c.s_m + (long)n * c.s_n] : 0.f;
-  const float whole = expm1f((float)tokens * g);
+  const Kept whole = kept(tokens, g);
   float* at = c.states + (long)bh * p.nseg * per + (long)m * c.st_m + (long)n * c.st_n;
   for (int s = 0; s < p.nseg; s += U) {
     float add[U];
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p
       if (s + u >= p.nseg) break;
       at[(long)u * per] = x;
       const int k = min(max(len - (s + u) * tokens, 0), tokens);
-      if (k > 0) x = fmaf(x, k == tokens ? whole : expm1f((float)k * g), x) + add[u];
+      if (k > 0) x = (k == tokens ? whole : kept(k, g))(x) + add[u];
     }
     at += (long)U * per;
   }
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
   }
   __syncthreads();
   const int c = t % per_row, g = t / per_row, groups = 256 / per_row, n0 = c * 4, D = a.Dv;
-  const float decay = exp2f(a.log_decay[h] * kLog2e);
+  const Kept decay = kept(1, a.log_decay[h]);
   const float* in = a.s0 + (long)blockIdx.x * a.Dk * D;
   float* out = a.sT + (long)blockIdx.x * a.Dk * D;
   float v[4], o[4] = {};
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[j] = decay * s[j] + k * v[j];
+      s[j] = fmaf(k, v[j], decay(s[j]));
       o[j] += q * s[j];
     }
     if (n0 + 4 <= D) {
@@ -142,11 +142,14 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
 // other lengths (6 ragged ones of up to 4095, 8 heads of 96, fp16 backward: 541
 // us, 592 without; but 1x65537, 16 heads of 128: 472 with twice as many, whose
 // states are then a sixth of the traffic, and 451 without). No segment is below
-// eight chunks. The same for a state and its transpose.
+// four chunks, and two are none: 1x1024, 8 heads of 64, bf16 forward takes 22 us
+// and 31 with eight chunks at least, 2x256 22 in two segments and 18 in one. The
+// same for a state and its transpose.
 Split split_of(int B, int T, int H, int M, int N) {
   const int all = std::max(1, ceil_div(T, kChunk));
   const long units = std::max(1l, (long)B * H * ceil_div(std::max(M, N), 64)), want = (all <= 256 ? 8l : 4l) * plan_cus();
-  const long nseg = std::max(1l, units >= 2l * plan_cus() ? 1 : std::min((want + units - 1) / units, (long)all / 8));
+  long nseg = units >= 2l * plan_cus() ? 1 : std::min((want + units - 1) / units, (long)all / 4);
+  if (nseg < 3) nseg = 1;
   const int chunks = ceil_div(all, nseg);
   return Split{ceil_div(all, chunks), chunks};
 }

@@ -27,10 +27,18 @@ def acc(prec, T):
     return (320 + T / 32) * 2.0 ** -24 + (0 if prec == "fp32" else 3 * 2.0 ** -16)
 
 
+def near_stored(got, ref, bound, prec, name):
+    """near, where what rounds beyond fp16's largest number is stored as an
+    infinity: from 65520 on, half a step above it."""
+    beyond = (prec == "fp16") & (np.abs(ref) + bound >= 65520) & np.isinf(got) & (np.sign(got) == np.sign(ref))
+    near(np.where(beyond, ref, got), ref, bound, name)
+
+
 def decays(H, kind="mixed"):
     with np.errstate(divide="ignore"):
         return np.log1p(-np.exp2(-np.arange(1, H + 1, dtype=np.float64))).astype(np.float32) if kind == "mixed" else \
-            np.array({"ends": [-np.inf, 0.0, -80.0, -1e-4]}[kind] * H, np.float32)[:H]
+            np.array({"ends": [-np.inf, 0.0, -80.0, -1e-4], "growing": [0.01, -0.5, 0.1, 1e-5]}[kind] * H,
+                     np.float32)[:H]
 
 
 def ints(a):
@@ -110,7 +118,7 @@ class Case:
         ao, As, _ = linattn.forward(*args(np.abs), self.g, lens, None if self.s0 is None else np.abs(self.s0),
                                     self.scale)
         got = self.rows(o, self.sizes[5])
-        near(got[on], ro[on], U[self.prec] * np.abs(ro[on]) + tol * ao[on] + TINY[self.prec], "o")
+        near_stored(got[on], ro[on], U[self.prec] * np.abs(ro[on]) + tol * ao[on] + TINY[self.prec], self.prec, "o")
         assert np.all(got[~on] == 7.0) and gaps_kept(o, buf)
         near(f64(sT).reshape(rs.shape), rs, tol * As + 1e-37, "sT")
 
@@ -124,7 +132,7 @@ class Case:
         ref, size = f(lambda x: x), f(np.abs)
         for n, r, s, w in zip(("dq", "dk", "dv"), ref, size, (self.sizes[4], self.sizes[4], self.sizes[5])):
             got = self.rows(outs[n][0], w)
-            near(got[on], r[on], U[self.prec] * np.abs(r[on]) + tol * s[on] + TINY[self.prec], n)
+            near_stored(got[on], r[on], U[self.prec] * np.abs(r[on]) + tol * s[on] + TINY[self.prec], self.prec, n)
             assert np.all(got[~on] == 7.0) and gaps_kept(*outs[n]), n
         near(f64(ds0).reshape(ref[3].shape), ref[3], tol * size[3] + 1e-37, "ds0")
 
@@ -137,7 +145,8 @@ CASES = [(1, 1, 1, 1, 1, 1, None, True, 0, 0), (2, 1, 3, 1, 5, 7, None, False, 0
          (1, 257, 1, 1, 128, 200, None, False, 0, 0), (4, 77, 4, 4, 17, 33, [500, -3, 77, 32], True, 1, 3),
          (2, 196, 8, 8, 64, 64, None, False, 0, 0), (1, 500, 4, 1, 128, 128, None, True, 8, 8),
          (2, 33, 2, 2, 250, 3, [31, 33], True, 0, 0), (1, 40, 1, 1, 3, 250, None, True, 0, 0),
-         (2, 130, 2, 2, 129, 65, [130, 100], True, 0, 0)]
+         (2, 130, 2, 2, 129, 65, [130, 100], True, 0, 0), (1, 200, 2, 2, 64, 200, None, True, 0, 0),
+         (1, 70, 1, 1, 200, 130, None, True, 1, 0), (70, 40, 2, 2, 16, 16, None, False, 0, 0)]
 
 
 @pytest.mark.parametrize("prec", PRECS)
@@ -161,6 +170,21 @@ def test_decays_at_their_ends(prec, T, lengths):
     c = Case(prec, 2, T, 4, 2, 24, 40, lengths, True, kind="ends")
     c.check_fwd()
     c.check_bwd()
+
+
+@pytest.mark.parametrize("prec", PRECS)
+def test_growing_heads(prec):
+    """exp(0.1 * 150) = 3e6, in one segment and in several; and a head whose
+    state loses more than a chunk keeps, whose small rest counts."""
+    for T in (150, 500):
+        c = Case(prec, 1, T, 4, 4, 24, 40, None, True, kind="growing", size=0.01 if T > 200 else 1.0)
+        if T > 200:
+            c.g = np.minimum(c.g, 0.02).astype(np.float32)
+            c.gd = vec(c.g)
+        if prec == "fp16":
+            c.scale *= 2.0 ** -20
+        c.check_fwd()
+        c.check_bwd()
 
 
 @pytest.mark.parametrize("prec,T,Dk,Dv", [("bf16", 3001, 64, 64), ("fp32", 2500, 40, 24), ("fp16", 2049, 128, 16),
