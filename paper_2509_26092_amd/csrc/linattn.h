@@ -127,9 +127,9 @@ template <int P> struct Ops16 {
       for (int j = B - 1; j >= 0; --j)
         if (i + j < LIM) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8(a.p[i]), v8(b.p[j]), acc, 0, 0, 0);
   }
-  // The leading parts of two values, which keep the rest (exact: one product
-  // with -1 and one with 0 each, in place of a shift or mask and a difference;
-  // what is not finite reaches its neighbour, which is of the same sum always).
+  // The leading parts of two values of one sum, which keep the rest (exact: one
+  // product with -1 and one with 0 each, in place of a shift or mask and a
+  // difference; so what is not finite reaches the other value).
   // The factors go through registers: as literals, {-1, 0} was encoded as an
   // inline constant that the unit reads as {0, -1}.
   __device__ static inline uint32_t take(float& a, float& b) {
@@ -241,9 +241,9 @@ struct Tile {
 };
 
 // The 16 bytes of a row at p, its column `col`; zeros for columns from `width`
-// on, and where the row is not there. A partial last chunk is
-// read from before its place and shifted. (No branch stands around a load: the
-// compiler would wait there for each.)
+// on, and where the row is not there. A partial last chunk is read from before
+// its place (see shift_part). (No branch stands around a load: the compiler
+// would wait there for each.)
 template <typename T, int WIDTHS>
 __device__ inline uint4 load_part(const T* p, int col, int width, bool there) {
   constexpr int VW = TT<T>::VW;
@@ -276,11 +276,15 @@ __device__ inline void put(typename OpsOf<T>::type::lds_t* p, int step, const ui
   if constexpr (OpsOf<T>::type::NP == 1) {
     *(uint4*)p = q;
   } else {
-    float v[8];
+    // (neighbours are of different columns: each part by itself)
+    float v[8], w[8];
     unpack<T>(q, v);
-    const auto f = OpsOf<T>::type::template parts<2>(v);
-    *(uint4*)p = f.p[0];
-    *(uint4*)(p + step) = f.p[1];
+    const uint4 lead = pack<bf16_t>(v);
+    unpack<bf16_t>(lead, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] -= w[i];
+    *(uint4*)p = lead;
+    *(uint4*)(p + step) = pack<bf16_t>(v);
   }
 }
 

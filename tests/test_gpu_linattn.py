@@ -390,4 +390,5 @@ def test_what_a_token_holds_reaches_no_earlier_one(prec, what, value):
         assert bad[37:].all()
     else:
         assert bad[37:, 3].all()
-        near(f64(o[0, :, 1, 4:]), ref[:, 4:], two[:, 4:], "other columns")
+        others = [n for n in range(48) if n != 3]
+        near(f64(o[0, :, 1])[:, others], ref[:, others], two[:, others], "other columns")
