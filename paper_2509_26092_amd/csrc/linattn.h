@@ -301,7 +301,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
   constexpr int C = kChunk, CT = C / 16, VW = TT<T>::VW, MT = MP / 16, KB = O::KB, KT = KB / 16, NP = O::NP;
   constexpr int PER_M = MP / VW, PER_N = TI::NB / VW, ROWS_M = 64 * W / PER_M, ROWS_N = 64 * W / PER_N;
   constexpr int NQ = ROWS_M > C ? 1 : C / ROWS_M, NV = C / ROWS_N;
-  static_assert(ROWS_M * PER_M == 64 * W && ROWS_N * PER_N == 64 * W && (NQ * ROWS_M == C || NQ == 1) && NV * ROWS_N == C, "loads");
+  static_assert(ROWS_M * PER_M == 64 * W && ROWS_N * PER_N == 64 * W && (NQ * ROWS_M == C || NQ == 1) && NV * ROWS_N == C,
+                "loads");
   __shared__ uint4 smem[TI::BYTES / 16];
   L* const sQ = (L*)smem;
   L* const sK = sQ + TI::OFF_K;

@@ -43,43 +43,57 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p
 
 // The gradients of query heads that share a key head, added up in the order
 // of the heads: part fp32 [tokens][H][N] to out [tokens][H / group][N]; dk and dv
-// in one launch.
+// in one launch. Bound by reading the parts (19 us for 6x4095 tokens of 8 heads
+// over 2, 96 and 100 columns).
 struct GroupSum {
   const float* part[2];
   void* out[2];
   long ldo[2];
   int N[2];
 };
-// V columns a thread, tiles of 16 rows a block.
+// V columns a thread at a time, kGroupRun times in a block's run of columns.
+// (4: 266 us for that whole backward pass; 16, which are too few blocks, 287.)
+constexpr int kGroupRun = 4;
 template <typename T, int V>
 __global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, const int32_t* lengths, int B, int T_, int H,
                                                                 int group) {
-  const int w = blockIdx.y, N = a.N[w], Hk = H / group, units = Hk * N / V;
-  const long rows = (long)B * T_;
-  for (long r0 = blockIdx.x * 16l; r0 < rows; r0 += gridDim.x * 16l)
-    for (int e = threadIdx.x; e < 16 * units; e += 256) {
-      const long row = r0 + e / units;
-      if (row >= rows || (lengths && (int)(row % T_) >= lengths[row / T_])) continue;
-      const int col = e % units * V, hk = col / N;
-      const float* p = a.part[w] + (row * H + (long)hk * group) * N + (col - hk * N);
-      float s[V];
-      __builtin_memcpy(s, p, sizeof(s));
+  const int w = blockIdx.y, N = a.N[w], Hk = H / group;
+  const unsigned units = (unsigned)Hk * N / V, rows = (unsigned)B * T_;   // below 2^28 and 2^31
+  const long total = (long)rows * units, run = 256 * kGroupRun;
+  for (long e0 = blockIdx.x * run + threadIdx.x; e0 < total; e0 += gridDim.x * run) {
+    unsigned row = (unsigned)(e0 / units), u = (unsigned)(e0 - (long)row * units);
+    for (int i = 0; i < kGroupRun && row < rows; ++i) {
+      if (!lengths || (int)(row % T_) < lengths[row / T_]) {
+        const int col = (int)u * V, hk = col / N;
+        const float* p = a.part[w] + ((long)row * H + (long)hk * group) * N + (col - hk * N);
+        float s[V];
+        __builtin_memcpy(s, p, sizeof(s));
 #pragma unroll 4
-      for (int g = 1; g < group; ++g) {
-        float t[V];
-        __builtin_memcpy(t, p + (long)g * N, sizeof(t));
+        for (int g = 1; g < group; ++g) {
+          float t[V];
+          __builtin_memcpy(t, p + (long)g * N, sizeof(t));
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] += t[j];
+          for (int j = 0; j < V; ++j) s[j] += t[j];
+        }
+        T o[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = TT<T>::from_f(s[j]);
+        __builtin_memcpy((T*)a.out[w] + (long)row * a.ldo[w] + col, o, sizeof(o));
       }
-      T o[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) o[j] = TT<T>::from_f(s[j]);
-      __builtin_memcpy((T*)a.out[w] + row * a.ldo[w] + col, o, sizeof(o));
+      u += 256;
+      if (u >= units) {
+        row += u / units;
+        u %= units;
+      }
     }
+  }
 }
 
 // One token: a block per sequence and head, a lane per four columns of the
-// state and group of its rows; bound by reading and writing the state.
+// state and group of its rows. It does 4 operations for each 8 bytes, so it is
+// bound by reading and writing the state: 256 sequences, 16 heads of 128x128 (537
+// MB) take 111 us, 4.8 TB/s of a copy's 5.2; one sequence, 8 heads of 64 5 us, which
+// is a launch and three dependent passes.
 template <typename T>
 __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per_row) {
   __shared__ float sq[256], sk[256], part[16][260];
@@ -237,13 +251,15 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   const long rows = (long)a.B * a.T;
   if (r || G == 1 || rows <= 0) return r;
   const GroupSum gs{{pk, pv}, {a.dk, a.dv}, {a.lddk, a.lddv}, {a.Dk, a.Dv}};
-  const dim3 grid((unsigned)std::min((rows + 15) / 16, 32768l), 2);
+  const long units = rows * (a.H / G) * std::max(a.Dk, a.Dv);
   return with_prec(prec, [&](auto tag) {
     using T = decltype(tag);
+    constexpr long run = 256 * kGroupRun;
+    auto grid = [&](int V) { return dim3((unsigned)std::min((units / V + run - 1) / run, 32768l), 2); };
     if (a.Dk % 4 == 0 && a.Dv % 4 == 0)
-      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 4>), grid, dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
+      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 4>), grid(4), dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
     else
-      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 1>), grid, dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
+      hipLaunchKernelGGL((linattn_group_sum_kernel<T, 1>), grid(1), dim3(256), 0, s, gs, a.lengths, a.B, a.T, a.H, G);
     return launched();
   });
 }

@@ -6,7 +6,17 @@
 //   xh = h rstd, g = dy gamma, dh = rstd (g - xh sum(g xh) / D) + dr,
 //   dx = m dh, dgamma = sum over rows of dy xh
 // The norm takes h as it is stored, which is what the backward pass sees.
-// The mask is computed again from its counter wherever it is needed.
+// The mask is computed again from its counter wherever it is needed: it costs
+// about 30 integer instructions for four elements and no memory.
+//
+// Bound by memory where rows are many, by the launch where they are few (64x512
+// takes 3 us in each kernel). So a row is read once and written from registers,
+// and the sum, the scaling and the residual's addition share that pass. HBM
+// rates, of the 5.2 TB/s of a plain copy:
+//   forward to 8 bits, bf16 16384x8192 with residual: 177 us for 940 MB
+//   backward, bf16 50176x512 with dropout and residual: 51 us for 257 MB, and
+//     5 us for the launch that joins dgamma's partial sums
+//   dropout, fp16 16385x2050 with residual, rows of odd strides: 45 us for 202 MB
 #include <math.h>
 
 #include "philox.h"
@@ -18,7 +28,7 @@ namespace {
 
 // ------------------------------------------------------------------ dropout
 // A thread takes chunks of 16 bytes, a grid's width apart: their rows and
-// places follow by addition from the first one's.
+// places follow by addition from the first one's, without a division each.
 template <typename T, bool RES>
 __global__ __launch_bounds__(256) void dropout_rows_kernel(const T* x, const T* res, T* y, long R, int D, long ldx,
                                                            long ldres, long ldy, Dropout d) {
@@ -722,7 +732,10 @@ size_t rmsnorm_bwd_workspace(int prec, long R, int D) {
 
 // Calls whose dgamma blocks of their own add up, in place of a second launch that
 // joins partial sums; dy and h are read twice, from cache, and a column's sum is
-// a chain of R / 32 additions.
+// a chain of R / 32 additions. A call so and with the second launch (us, its own
+// 3 to 5 among them): fp32 64x512 7.4 and 10.4, 1024x2048 (8 MB) 11.9 and 12.3,
+// bf16 1024x4096 (8 MB) 13.6 and 15.6; beyond the rule fp32 1024x4096 19.0 and
+// 17.2, 2048x512 13.6 and 10.6, bf16 512x16384 36.3 and 32.8.
 static bool rms_bwd_small(int prec, long R, int D) {
   return R <= 1024 && R * D * prec_bytes(prec) <= (8l << 20);
 }

@@ -392,3 +392,23 @@ def test_what_a_token_holds_reaches_no_earlier_one(prec, what, value):
         assert bad[37:, 3].all()
         others = [n for n in range(48) if n != 3]
         near(f64(o[0, :, 1])[:, others], ref[:, others], two[:, others], "other columns")
+
+
+def test_as_many_heads_as_there_may_be():
+    """2^20 query heads over 2^19 key heads, one token: rows of 2^28 elements.
+    Small integers, whose products and sums are exact."""
+    import torch
+    H, Hk, Dk, Dv, P = 1 << 20, 1 << 19, 256, 1, PREC["bf16"]
+    sizes = (1, 1, H, Hk, Dk, Dv)
+    small = lambda n, w: torch.randint(-3, 4, (n, w), device="cuda", dtype=torch.int8).to(torch.bfloat16)
+    q, k, v, do = small(H, Dk), small(Hk, Dk), small(Hk, Dv), small(H, Dv)
+    g = torch.zeros(H, device="cuda")
+    dq, dk, dv = (torch.full_like(x, 7) for x in (q, k, v))
+    ws = ws_of(B.rn18op_linattn_bwd_workspace(P, *sizes))
+    B.rn18op_linattn_bwd(P, q, k, v, do, g, None, None, None, dq, dk, dv, None, *sizes, H * Dk, Hk * Dk, Hk * Dv,
+                         H * Dv, H * Dk, Hk * Dk, Hk * Dv, 1.0, ws)
+    shared = lambda x: x.view(Hk, 2, 1)
+    assert torch.equal(dq.view(Hk, 2, Dk), shared(do) * v.view(Hk, 1, 1) * k.view(Hk, 1, Dk))
+    assert torch.equal(dk, (q.view(Hk, 2, Dk) * (shared(do) * v.view(Hk, 1, 1))).sum(1))
+    dots = (q.view(Hk, 2, Dk).float() * k.view(Hk, 1, Dk).float()).sum(2, keepdim=True)
+    assert torch.equal(dv, (dots * shared(do).float()).sum(1).to(torch.bfloat16))
