@@ -80,18 +80,18 @@ int rn18op_round_bf16(const float* x, uint16_t* y, size_t n, void* hip_stream);
 
 /* ---- Row operators -------------------------------------------------------
  * Layer norm, RMS norm, dropout, a teacher's top logits and the distillation
- * loss work on R rows
- * of a matrix whose rows are `ld` elements apart (ld >= the width; any ld, any
- * width from 1 to 2^30). Their tensors of the storage type need only the alignment
- * of one element, their fp32 and int32 arrays that of 4 bytes; rows may be of
- * any number whose tensors span at most 2^46 elements, R = 0 included. `prec`
- * may be RN18_FP16 too. Sums, statistics and the loss are fp32 or wider, and
- * what is stored in 16 bits is rounded once, to nearest even. An output of
- * the storage type may be an input itself (the same pointer and row stride);
- * tensors must not overlap otherwise. Results do not depend on the order in
- * which blocks run: the same inputs give the same bits. A workspace is
- * scratch of one call (16-byte aligned, NULL where 0 bytes are needed): calls
- * that may overlap need one each. RN18_ENOMEM if it is too small. */
+ * loss work on R rows of a matrix whose rows are `ld` elements apart (ld >=
+ * the width; any ld, any width from 1 to 2^30). Their tensors of the storage
+ * type need only the alignment of one element, their fp32 and int32 arrays
+ * that of 4 bytes; rows may be of any number whose tensors span at most 2^46
+ * elements, R = 0 included. `prec` may be RN18_FP16 too. Sums, statistics and
+ * the loss are fp32 or wider, and what is stored in 16 bits is rounded once,
+ * to nearest even. An output of the storage type may be an input itself (the
+ * same pointer and row stride); tensors must not overlap otherwise. Results
+ * do not depend on the order in which blocks run: the same inputs give the
+ * same bits. A workspace is scratch of one call (16-byte aligned, NULL where
+ * 0 bytes are needed): calls that may overlap need one each. RN18_ENOMEM if
+ * it is too small. */
 
 /* Layer norm over the D channels of each row (one pixel of an NHWC tensor):
  *   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),
@@ -224,11 +224,13 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
  * into [0, T]): tokens from a sequence's length on are neither read nor
  * written. States are fp32 [B][H][Dk][Dv], dense: s0 before the first token
  * (NULL: zeros), sT after the last (NULL: not wanted; may be s0 itself). Dk
- * and Dv from 1 to 256, B T H up to 2^31 - 1, B H up to 2^20, T up to 2^26. Sums and states
- * are fp32; the products of 16-bit types keep the decayed and summed operands
- * in parts of 8 bits that add up to 16 bits or more, and o is rounded once.
- * Outputs overlap no input but for sT. Results do not depend on the order in
- * which blocks run. Workspaces are those of the row operators. */
+ * and Dv from 1 to 256, B T H up to 2^31 - 1, B H up to 2^20, T up to 2^26.
+ * Sums and states are fp32; the products of 16-bit types keep the decayed and
+ * summed operands in parts of 8 bits that add up to 16 bits or more, and o is
+ * rounded once. A NaN or an infinity changes nothing before its token; from
+ * there on it may make a sequence's head NaN, but one in v, or in the state, only
+ * its column. Outputs overlap no input but for sT. Results do not depend on the
+ * order in which blocks run. Workspaces are those of the row operators. */
 size_t rn18op_linattn_fwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
 int rn18op_linattn_fwd(int prec, const void* q, const void* k, const void* v, const float* log_decay,
                        const int32_t* lengths, const float* s0, void* o, float* sT, int B, int T, int H, int Hk, int Dk,
