@@ -105,6 +105,17 @@ __device__ inline int seq_len(const Core& c, int b) {
 // held as two parts each (exact), what is computed in fp32 (X, the scores, the
 // decayed v) as two or three. Products of parts below 2^-16 of the result are
 // left out, for the state 2^-24.
+//
+// Bound by the vector units (parts of X and the scores, decay of X), the matrix
+// units and memory, which two waves of a SIMD overlap only in part. bf16 forward:
+// 256x196 tokens, 8 heads of 64, 66 us for 239 MB of HBM (3.6 TB/s of a copy's
+// 5.2); 1x65537, 16 heads of 128, 340 us for 1.1 GB (the vector units are busy for
+// 48% of that, the matrix units for 31%) after 140 us for the segments' sums (561
+// MB, 4.0 TB/s); bf16 backward of the first, three passes, 140 us for 455 MB.
+// Slower or no faster: three waves of a SIMD (X leaves no room for them in the
+// registers), loads two chunks ahead (80 us and 67 for the first), rows in LDS 8 or
+// 12 banks further each, tables of the powers in LDS, a higher priority of waves
+// that load (434 and 436 us for all of the second).
 
 // A lane's operand of one step over KB of the inner index, in NP parts: places
 // 4 (lane / 16) + 0..3 of the first and of the second 16 in 16 bits, of 16 in
@@ -510,29 +521,34 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) out[it][nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
       }
+      // (one body for all of the inner index: 426 us in place of 434 with a branch
+      // in each step, 1x65537 tokens, 16 heads of 128, bf16 forward)
+      auto products = [&](auto with_state) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kb = 0; kb < MP / KB; ++kb) {
-        typename O::In q[CT];
-        typename O::Two A[NT];
+        for (int kb = 0; kb < MP / KB; ++kb) {
+          typename O::In q[CT];
 #pragma unroll
-        for (int it = 0; it < CT; ++it) q[it] = frag_row(sQ, 16 * it, kb * KB);
+          for (int it = 0; it < CT; ++it) q[it] = frag_row(sQ, 16 * it, kb * KB);
 #pragma unroll
-        for (int jt = 0; jt < CT; ++jt) {
-          const auto k = frag_row(sK, 16 * jt, kb * KB);
+          for (int jt = 0; jt < CT; ++jt) {
+            const auto k = frag_row(sK, 16 * jt, kb * KB);
 #pragma unroll
-          for (int it = jt; it < CT; ++it) O::template mma<2>(P[it][jt], k, q[it]);
+            for (int it = jt; it < CT; ++it) O::template mma<2>(P[it][jt], k, q[it]);
+          }
+          if constexpr (decltype(with_state)::value)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              float x[O::EV];
+#pragma unroll
+              for (int e = 0; e < O::EV; ++e) x[e] = X[kb * KT + e / 4][nt][e % 4];
+              const typename O::Two A = O::template parts<2>(x);
+#pragma unroll
+              for (int it = 0; it < CT; ++it) O::template mma<2>(out[it][nt], A, q[it]);
+            }
         }
-        if (empty) continue;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float x[O::EV];
-#pragma unroll
-          for (int e = 0; e < O::EV; ++e) x[e] = X[kb * KT + e / 4][nt][e % 4];
-          A[nt] = O::template parts<2>(x);
-#pragma unroll
-          for (int it = 0; it < CT; ++it) O::template mma<2>(out[it][nt], A[nt], q[it]);
-        }
-      }
+      };
+      if (empty) products(std::false_type());
+      else products(std::true_type());
 #pragma unroll
       for (int it = 0; it < CT; ++it) {
 #pragma unroll
