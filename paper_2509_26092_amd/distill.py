@@ -54,6 +54,11 @@ def _rows(t):
     return t, t.stride(0) if r > 1 else d
 
 
+def _workspace(need):
+    """Scratch of one call: no other stream's, and of a captured call its graph's own."""
+    return torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+
+
 class LayerNorm:
     """Layer norm over the last axis of [rows][width]: parameters, what the
     backward pass needs, and gradients."""
@@ -61,7 +66,6 @@ class LayerNorm:
     def __init__(self, width):
         self.gamma, self.beta = torch.ones(width, device="cuda"), torch.zeros(width, device="cuda")
         self.dgamma, self.dbeta = torch.empty_like(self.gamma), torch.empty_like(self.beta)
-        self.ws = None
 
     def forward(self, x):
         r, d = x.shape
@@ -82,11 +86,9 @@ class LayerNorm:
         if dy.shape != self.x.shape or dy.dtype != self.x.dtype:
             raise ValueError("a gradient of another shape or type than the forward pass's input")
         dy, ld = _rows(dy)
-        need = B.rn18op_layernorm_bwd_workspace(self.prec, r, d)
-        if self.ws is None or self.ws.numel() < need:
-            self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        ws = _workspace(B.rn18op_layernorm_bwd_workspace(self.prec, r, d))
         B.rn18op_layernorm_bwd(self.prec, dy, self.x, self.gamma, self.mean, self.rstd, dy, self.dgamma, self.dbeta, r,
-                               d, ld, self.ldx, ld, self.ws)
+                               d, ld, self.ldx, ld, ws)
         return dy
 
 
@@ -115,7 +117,7 @@ class RmsNorm:
     def __init__(self, width, layer, dropout):
         self.gamma = torch.ones(width, device="cuda")
         self.dgamma = torch.empty_like(self.gamma)
-        self.layer, self.dropout, self.ws = layer, dropout, None
+        self.layer, self.dropout = layer, dropout
 
     def _random(self, p):
         return dict(p=p, seed=self.dropout.seed, step=self.layer << 48, step_add=self.dropout.steps)
@@ -123,6 +125,10 @@ class RmsNorm:
     def forward(self, x, res=None, train=True):
         """(h, y): the stream behind the addition, and its norm."""
         r, d = x.shape
+        if d != len(self.gamma):
+            raise ValueError("rows of %d elements for a norm of %d" % (d, len(self.gamma)))
+        if res is not None and (res.shape != x.shape or res.dtype != x.dtype):
+            raise ValueError("a residual of another shape or type than the branch")
         x, ldx = _rows(x)
         self.p = self.dropout.p if train and res is not None else 0.0
         h, ldres = (x, 0) if res is None else (torch.empty((r, d), dtype=x.dtype, device=x.device), d)
@@ -139,16 +145,17 @@ class RmsNorm:
     def backward(self, dy, dr=None):
         """(gradient of the residual, gradient of the branch) from y's gradient
         and what else the stream's receives."""
+        for g in (dy, dr):
+            if g is not None and (g.shape != self.h.shape or g.dtype != self.h.dtype):
+                raise ValueError("a gradient of another shape or type than the forward pass's input")
         r, d = dy.shape
         dy, lddy = _rows(dy)
         dr, lddr = _rows(dr) if dr is not None else (None, 0)
-        need = B.rn18op_rmsnorm_bwd_workspace(_prec(dy), r, d)
-        if self.ws is None or self.ws.numel() < need:
-            self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        ws = _workspace(B.rn18op_rmsnorm_bwd_workspace(_prec(dy), r, d))
         dh = torch.empty((r, d), dtype=dy.dtype, device=dy.device)
         dx = torch.empty_like(dh) if self.p > 0 else None
         B.rn18op_rmsnorm_bwd(_prec(dy), dy, dr, self.h, self.gamma, self.rstd, dh, dx, self.dgamma, r, d, lddy, lddr,
-                             self.ldh, d, d, ws=self.ws, **self._random(self.p))
+                             self.ldh, d, d, ws=ws, **self._random(self.p))
         return dh, dh if dx is None else dx
 
 
@@ -164,23 +171,19 @@ class Mixer:
         self.wo = torch.randn((width, width), device="cuda", generator=generator) * width ** -0.5
         # each head looks back twice as far as the one before it
         self.log_decay = torch.log1p(-torch.exp2(-1.0 - torch.arange(heads, device="cuda", dtype=torch.float32)))
-        self.ws = None
-
-    def _workspace(self, need):
-        if need and (self.ws is None or self.ws.numel() < need):
-            self.ws = torch.empty(need, dtype=torch.uint8, device="cuda")
-        return self.ws if need else None
 
     def _parts(self, qkv):
         return [qkv[:, i * self.width:(i + 1) * self.width] for i in range(3)]
 
     def forward(self, y, n):
         """The branch of the rows y: n sequences one after the other."""
+        if len(y) % n:
+            raise ValueError("%d rows of %d sequences" % (len(y), n))
         self.y, self.sizes = y, (n, len(y) // n, self.heads, self.heads, self.dim, self.dim)
         self.qkv = y @ self.wqkv.to(y.dtype)
         self.o = torch.empty((len(y), self.width), dtype=y.dtype, device=y.device)
         ld, p = self.qkv.stride(0), _prec(y)
-        ws = self._workspace(B.rn18op_linattn_fwd_workspace(p, *self.sizes))
+        ws = _workspace(B.rn18op_linattn_fwd_workspace(p, *self.sizes))
         B.rn18op_linattn_fwd(p, *self._parts(self.qkv), self.log_decay, None, None, self.o, None, *self.sizes, ld, ld, ld,
                              self.width, self.dim ** -0.5, ws)
         return self.o @ self.wo.to(y.dtype)
@@ -190,7 +193,7 @@ class Mixer:
         self.dwo = (self.o.t() @ dx).float()
         do = dx @ self.wo.to(dx.dtype).t()
         dqkv, p, ld = torch.empty_like(self.qkv), _prec(dx), self.qkv.stride(0)
-        ws = self._workspace(B.rn18op_linattn_bwd_workspace(p, *self.sizes))
+        ws = _workspace(B.rn18op_linattn_bwd_workspace(p, *self.sizes))
         B.rn18op_linattn_bwd(p, *self._parts(self.qkv), do, self.log_decay, None, None, None, *self._parts(dqkv), None,
                              *self.sizes, ld, ld, ld, do.stride(0), ld, ld, ld, self.dim ** -0.5, ws)
         self.dwqkv = (self.y.t() @ dqkv).float()
@@ -217,6 +220,8 @@ class TokenStudent:
     features, logits and parameters in fp32."""
 
     def __init__(self, classes, width=512, patch=16, dtype=torch.bfloat16, seed=0, blocks=0, heads=8, dropout=0.0):
+        if dropout and not blocks:
+            raise ValueError("dropout without residual blocks, whose branches it drops")
         g = torch.Generator(device="cuda").manual_seed(seed)
         fan = 3 * patch * patch
         self.patch, self.dtype = patch, dtype
@@ -315,6 +320,8 @@ def run(student="tokens", arch="imagenet", classes=1000, batch=64, size=128, ste
         alpha=0.9, lr=0.005, prec="bf16", batches=4, log=None, blocks=0, heads=8, dropout=0.0):
     """Trains a student on a few synthetic batches against a network with
     random weights, whose targets are taken once; returns the losses."""
+    if student != "tokens" and (blocks or dropout):
+        raise ValueError("residual blocks and their dropout are the token student's")
     teacher = B.Worker(arch, classes, prec)
     state = torch.zeros(teacher.n_state, device="cuda")
     B.rn18_destroy(B.rn18_init(teacher.cfg, 1, state))

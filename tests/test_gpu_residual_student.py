@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import rows
-from paper_2509_26092_amd import inputs
+from paper_2509_26092_amd import binding as B, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,52 @@ def test_the_command_runs_with_blocks():
     from paper_2509_26092_amd import distill
     losses = distill.run("tokens", "cifar", 100, 8, 32, 4, prec="bf16", batches=2, blocks=2, heads=4, dropout=0.1)
     assert len(losses) == 4 and np.isfinite(losses).all()
+
+
+def test_a_captured_step_has_scratch_of_its_own():
+    """A captured step's workspaces are not those of eager steps, which a larger
+    batch would replace, so that replays would write to memory given back."""
+    import torch
+    from paper_2509_26092_amd import distill
+    make = lambda: distill.TokenStudent(20, width=128, patch=8, dtype=torch.float32, seed=4, blocks=1, heads=1)
+    data, larger = batch(2, 20, 3, (160, 160)), batch(3, 20, 3, (192, 192))
+    step = lambda s: s.train_step(*data, 2.0, 0.6, 0.02)
+    a, b = make(), make()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a), step(b)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        loss = step(b)
+    sizes = [B.rn18op_linattn_bwd_workspace(0, 2, 400, 1, 1, 128, 128), B.rn18op_rmsnorm_bwd_workspace(0, 800, 128)]
+    assert all(sizes)
+    with torch.cuda.stream(side):
+        b.gradients(*larger, 2.0, 0.6)
+        others = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        got, ref = loss.clone(), step(a)
+        torch.cuda.synchronize()
+        assert abs(got.item() - ref.item()) <= 1e-5 * abs(ref.item())
+        assert all((t == 7).all() for t in others)
+
+
+def test_the_layers_refuse_other_shapes_and_types():
+    import torch
+    from paper_2509_26092_amd import distill
+    d = distill.Dropout(0.0, 1)
+    norm, mixer = distill.RmsNorm(16, 1, d), distill.Mixer(16, 2, torch.Generator(device="cuda").manual_seed(1))
+    x = torch.ones((6, 16), device="cuda")
+    for args in ((x[:, :8],), (x, x[:3]), (x, x.bfloat16())):
+        with pytest.raises(ValueError):
+            norm.forward(*args)
+    norm.forward(x, x)
+    for args in ((x[:3],), (x.bfloat16(),), (x, x[:3]), (x, x.bfloat16())):
+        with pytest.raises(ValueError):
+            norm.backward(*args)
+    with pytest.raises(ValueError):
+        mixer.forward(x, 4)

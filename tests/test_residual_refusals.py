@@ -127,3 +127,12 @@ def test_the_binding_refuses_arrays_of_other_types_and_sizes():
         with pytest.raises(B.Rn18Error):
             B.rn18op_linattn_fwd(B.RN18_BF16, x, x, x, kw["g"], kw["lengths"], kw["s0"], x, kw["sT"], 2, 4, 2, 1, 8, 4,
                                  16, 8, 4, 8, 1.0)
+
+
+def test_the_student_refuses_dropout_that_nothing_would_take():
+    from paper_2509_26092_amd import distill
+    with pytest.raises(ValueError, match="without residual blocks"):
+        distill.TokenStudent(20, dropout=0.1)
+    for kw in ({"blocks": 1}, {"dropout": 0.1}):
+        with pytest.raises(ValueError, match="token student"):
+            distill.run("resnet", **kw)
