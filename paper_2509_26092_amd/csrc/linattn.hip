@@ -89,8 +89,8 @@ __global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, cons
   }
 }
 
-// One token: a block per sequence and head, a lane per four columns of the
-// state and group of its rows. It does 4 operations for each 8 bytes, so it is
+// One token: a block per sequence, head and part of the state's columns, a lane
+// per four columns and group of the state's rows. It does 4 operations for each 8 bytes, so it is
 // bound by reading and writing the state: 256 sequences, 16 heads of 128x128 (537
 // MB) take 111 us, 4.8 TB/s of a copy's 5.2; one sequence, 8 heads of 64 5 us, which
 // is a launch and three dependent passes.
@@ -103,7 +103,8 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
     sk[t] = TT<T>::to_f(((const T*)a.k)[b * a.ldk + (long)hk * a.Dk + t]);
   }
   __syncthreads();
-  const int c = t % per_row, g = t / per_row, groups = 256 / per_row, n0 = c * 4, D = a.Dv;
+  const int c = t % per_row, g = t / per_row, groups = 256 / per_row, D = a.Dv;
+  const int first = blockIdx.y * per_row * 4, place = c * 4, n0 = first + place, here = min(D - first, per_row * 4);
   const Kept decay = kept(1, a.log_decay[h]);
   const float* in = a.s0 + (long)blockIdx.x * a.Dk * D;
   float* out = a.sT + (long)blockIdx.x * a.Dk * D;
@@ -135,19 +136,19 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) part[g & 15][n0 + j] = 0.f;
+  for (int j = 0; j < 4; ++j) part[g & 15][place + j] = 0.f;
   __syncthreads();
   // the row groups' sums: by sixteens in order where there are more of them
   for (int p = 0; p < groups; p += 16) {
     if (g / 16 == p / 16)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) part[g & 15][n0 + j] += o[j];
+      for (int j = 0; j < 4; ++j) part[g & 15][place + j] += o[j];
     __syncthreads();
   }
-  for (int n = t; n < D; n += 256) {
+  for (int n = t; n < here; n += 256) {
     float s = 0.f;
     for (int p = 0; p < min(groups, 16); ++p) s += part[p][n];
-    ((T*)a.o)[b * a.ldo + (long)h * D + n] = TT<T>::from_f(s);
+    ((T*)a.o)[b * a.ldo + (long)h * D + first + n] = TT<T>::from_f(s);
   }
 }
 
@@ -159,23 +160,33 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
 // four chunks, and two are none: 1x1024, 8 heads of 64, bf16 forward takes 22 us
 // and 31 with eight chunks at least, 2x256 22 in two segments and 18 in one. The
 // same for a state and its transpose.
-Split split_of(int B, int T, int H, int M, int N) {
-  const int all = std::max(1, ceil_div(T, kChunk));
+// No segments, whose sums are another pass over k and v, for heads that fill
+// the card by themselves, which a backward pass does sooner: its three passes
+// run side by side. us without segments and with them, where the rule begins,
+// backward: bf16 12x2048, 16 heads of 64 160 and 200, 11x1000, 8 heads of 128 134
+// and 176, fp32 12x1024, 16 of 128 634 and 764; below it bf16 16x3000, 8 of 64 228
+// and 196, fp32 (bound by the matrix units, which want more waves) 6x2048, 16 of
+// 128 814 and 728. Forward, sequences of up to 64 chunks: bf16 12x1024, 16 of 128
+// 88 and 135, 14x486 50 and 97; longer or fewer ones: 17x3000, 16 of 64 227 and
+// 134, 12x2048 106 and 99.
+Split split_of(int prec, int B, int T, int H, int M, int N, int passes) {
+  const int all = std::max(1, ceil_div(T, kChunk)), beside = passes == 1 ? 1 : prec == PREC_F32 ? 2 : 3;
   const long units = std::max(1l, (long)B * H * ceil_div(std::max(M, N), 64)), want = (all <= 256 ? 8l : 4l) * plan_cus();
-  long nseg = units >= 2l * plan_cus() ? 1 : std::min((want + units - 1) / units, (long)all / 4);
+  const long enough = passes == 1 && all <= 64 ? 3l * plan_cus() / 2 : 2l * plan_cus();
+  long nseg = units * beside >= enough ? 1 : std::min((want + units - 1) / units, (long)all / 4);
   if (nseg < 3) nseg = 1;
   const int chunks = ceil_div(all, nseg);
   return Split{ceil_div(all, chunks), chunks};
 }
-size_t split_bytes(int B, int T, int H, int M, int N) {
-  const Split p = split_of(B, T, H, M, N);
+size_t split_bytes(int prec, int B, int T, int H, int M, int N, int passes) {
+  const Split p = split_of(prec, B, T, H, M, N, passes);
   return p.nseg > 1 ? (size_t)B * H * p.nseg * M * N * 4 : 0;
 }
 
-int cores_launch(int prec, const Cores& cs, hipStream_t s) {
+int cores_launch(int prec, const Cores& cs, int passes, hipStream_t s) {
   const Core& c = cs.c[0];
   if (c.B <= 0) return 0;
-  const Split p = split_of(c.B, c.T, c.H, c.M, c.N);
+  const Split p = split_of(prec, c.B, c.T, c.H, c.M, c.N, passes);
   switch (prec) {
     case PREC_F32: return chunks_launch_fp32(cs, p, s);
     case PREC_BF16: return chunks_launch_bf16(cs, p, s);
@@ -193,8 +204,8 @@ int segments_launch(const Cores& cs, const Split& p, hipStream_t s) {
   return launched();
 }
 
-size_t linattn_fwd_workspace(int, int B, int T, int H, int, int Dk, int Dv) {
-  return split_bytes(B, T, H, Dk, Dv);
+size_t linattn_fwd_workspace(int prec, int B, int T, int H, int, int Dk, int Dv) {
+  return split_bytes(prec, B, T, H, Dk, Dv, 1);
 }
 
 int linattn_fwd_launch(int prec, const LinattnFwd& a, void* ws, hipStream_t s) {
@@ -203,16 +214,20 @@ int linattn_fwd_launch(int prec, const LinattnFwd& a, void* ws, hipStream_t s) {
   cs.c[0] = Core{{a.q, a.ldq, 1}, {a.k, a.ldk, G}, {a.v, a.ldv, G}, a.o, a.ldo, 0, a.log_decay, a.lengths, a.s0, a.sT,
                  a.Dv, 1, a.B, a.T, a.H, a.Dk, a.Dv, 0, a.scale, 1.f, (float*)ws, a.Dv, 1};
   cs.n = cs.sums = 1;
-  return cores_launch(prec, cs, s);
+  return cores_launch(prec, cs, 1, s);
 }
 
 int linattn_step_launch(int prec, const LinattnFwd& a, hipStream_t s) {
   if (a.B <= 0) return 0;
   int per_row = 1;
   while (per_row * 4 < a.Dv) per_row *= 2;
+  // a state's columns over several blocks where there are few states (us): 95
+  // sequences, 2 heads of 256 25 in place of 50 with a block each, 32, 8 heads of
+  // 256 32 of 55, 8, 16 heads of 128 8.5 of 10.5
+  while (per_row > 4 && (long)a.B * a.H * ceil_div(a.Dv, per_row * 4) < 4l * plan_cus()) per_row /= 2;
   return with_prec(prec, [&](auto tag) {
     using T = decltype(tag);
-    hipLaunchKernelGGL(linattn_step_kernel<T>, dim3(a.B * a.H), dim3(256), 0, s, a, per_row);
+    hipLaunchKernelGGL(linattn_step_kernel<T>, dim3(a.B * a.H, ceil_div(a.Dv, per_row * 4)), dim3(256), 0, s, a, per_row);
     return launched();
   });
 }
@@ -222,8 +237,8 @@ int linattn_step_launch(int prec, const LinattnFwd& a, hipStream_t s) {
 static size_t group_bytes(int B, int T, int H, int Hk, int D) {
   return H > Hk ? (((size_t)B * T * H * D * 4 + 255) & ~(size_t)255) : 0;
 }
-size_t linattn_bwd_workspace(int, int B, int T, int H, int Hk, int Dk, int Dv) {
-  return group_bytes(B, T, H, Hk, Dk) + group_bytes(B, T, H, Hk, Dv) + 2 * split_bytes(B, T, H, Dk, Dv);
+size_t linattn_bwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv) {
+  return group_bytes(B, T, H, Hk, Dk) + group_bytes(B, T, H, Hk, Dv) + 2 * split_bytes(prec, B, T, H, Dk, Dv, 3);
 }
 
 int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
@@ -233,7 +248,7 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   at += group_bytes(a.B, a.T, a.H, a.Hk, a.Dk);
   float* pv = (float*)at;
   at += group_bytes(a.B, a.T, a.H, a.Hk, a.Dv);
-  float *sf = (float*)at, *sr = (float*)(at + split_bytes(a.B, a.T, a.H, a.Dk, a.Dv));
+  float *sf = (float*)at, *sr = (float*)(at + split_bytes(prec, a.B, a.T, a.H, a.Dk, a.Dv, 3));
   const Operand q{a.q, a.ldq, 1}, k{a.k, a.ldk, G}, v{a.v, a.ldv, G}, d{a.dout, a.lddout, 1};
   // dq and dk: on the state's transpose, whose elements are taken the other way
   // round; dv goes with dk's segments. All in one launch where their kernel is
@@ -246,8 +261,8 @@ int linattn_bwd_launch(int prec, const LinattnBwd& a, void* ws, hipStream_t s) {
   const Core dv{k, q, d, G > 1 ? pv : a.dv, a.lddv, G > 1, a.log_decay, a.lengths, a.dsT, a.ds0, a.Dv, 1, a.B, a.T, a.H,
                 a.Dk, a.Dv, 1, 1.f, a.scale, sr, 1, a.Dk};
   const bool one = shape_of(prec, dq) == shape_of(prec, dv) && !(a.ds0 && a.ds0 == a.dsT);   // (dk reads dsT too)
-  int r = cores_launch(prec, one ? Cores{{dq, dk, dv}, 3, 2} : Cores{{dq, dk, dk}, 2, 2}, s);
-  if (!r && !one) r = cores_launch(prec, Cores{{dv, dv, dv}, 1, 0}, s);
+  int r = cores_launch(prec, one ? Cores{{dq, dk, dv}, 3, 2} : Cores{{dq, dk, dk}, 2, 2}, 3, s);
+  if (!r && !one) r = cores_launch(prec, Cores{{dv, dv, dv}, 1, 0}, 3, s);
   const long rows = (long)a.B * a.T;
   if (r || G == 1 || rows <= 0) return r;
   const GroupSum gs{{pk, pv}, {a.dk, a.dv}, {a.lddk, a.lddv}, {a.Dk, a.Dv}};

@@ -242,7 +242,8 @@ def test_states_in_place_and_not_wanted(T):
 @pytest.mark.parametrize("B_,H,Hk,Dk,Dv,pad,off", [(1, 1, 1, 1, 1, 0, 0), (1, 8, 8, 64, 64, 0, 0), (5, 4, 2, 96, 100, 3, 1),
                                                    (3, 2, 1, 256, 256, 0, 0), (2, 3, 3, 7, 250, 0, 5),
                                                    (2, 2, 2, 250, 6, 1, 0), (40, 16, 16, 128, 128, 0, 0),
-                                                   (2, 2, 2, 33, 13, 0, 0)])
+                                                   (2, 2, 2, 33, 13, 0, 0), (95, 2, 2, 40, 200, 0, 3),
+                                                   (300, 2, 1, 20, 130, 0, 0)])
 def test_step(prec, B_, H, Hk, Dk, Dv, pad, off):
     """Against the oracle's one token, into another state and in place."""
     import torch
