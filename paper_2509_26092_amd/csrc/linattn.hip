@@ -168,12 +168,16 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
 // and 196, fp32 (bound by the matrix units, which want more waves) 6x2048, 16 of
 // 128 814 and 728. Forward, sequences of up to 64 chunks: bf16 12x1024, 16 of 128
 // 88 and 135, 14x486 50 and 97; longer or fewer ones: 17x3000, 16 of 64 227 and
-// 134, 12x2048 106 and 99.
+// 134, 12x2048 106 and 99. A SIMD holds one wave of the widest states in place of
+// two, so that half as many heads of 129 columns or more fill the card: bf16
+// backward 4x1000, 8 of 256 170 and 321, forward 20x400, 4 of 256 78 and 139; half
+// of that forward, 4x1000, 165 and 128.
 Split split_of(int prec, int B, int T, int H, int M, int N, int passes) {
-  const int all = std::max(1, ceil_div(T, kChunk)), beside = passes == 1 ? 1 : prec == PREC_F32 ? 2 : 3;
+  const int all = std::max(1, ceil_div(T, kChunk)), beside = passes == 1 ? 1 : prec == PREC_F32 ? 2 : 3,
+            widest = std::max(M, N) > 128 ? 2 : 1;
   const long units = std::max(1l, (long)B * H * ceil_div(std::max(M, N), 64)), want = (all <= 256 ? 8l : 4l) * plan_cus();
   const long enough = passes == 1 && all <= 64 ? 3l * plan_cus() / 2 : 2l * plan_cus();
-  long nseg = units * beside >= enough ? 1 : std::min((want + units - 1) / units, (long)all / 4);
+  long nseg = units * beside * widest >= enough ? 1 : std::min((want + units - 1) / units, (long)all / 4);
   if (nseg < 3) nseg = 1;
   const int chunks = ceil_div(all, nseg);
   return Split{ceil_div(all, chunks), chunks};
