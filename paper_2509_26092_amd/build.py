@@ -13,8 +13,8 @@ SRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librn18.so")
 ARCH = os.environ.get("RN18_OFFLOAD_ARCH", "gfx950")
-SOURCES = ["conv.hip", "bn.hip", "misc.hip", "layernorm.hip",
-           "rmsnorm.hip", "linattn.hip", "linattn_fp32.hip", "linattn_bf16.hip", "linattn_fp16.hip", "topk.hip", "distill.hip", "api.cpp"]
+SOURCES = ["conv.hip", "bn.hip", "misc.hip", "layernorm.hip", "rmsnorm.hip", "linattn.hip", "linattn_fp32.hip",
+           "linattn_bf16.hip", "linattn_fp16.hip", "topk.hip", "distill.hip", "api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH,
          # packed-fp32 instructions are kept out of the generated code

@@ -481,7 +481,6 @@ __global__ __launch_bounds__(256) void ln_bwd_short_kernel(const T* dy, const T*
 
 // ------------------------------------------------------------------ rows beyond a block's registers
 // A block of 1024 threads per row reads it three times.
-// A block of 1024 threads per row reads it three times.
 template <typename T>
 __global__ __launch_bounds__(1024) void ln_fwd_long_kernel(const T* x, const float* __restrict__ gamma,
                                                            const float* __restrict__ beta, T* y,
