@@ -92,8 +92,8 @@ __global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, cons
 // One token: a block per sequence, head and part of the state's columns, a lane
 // per four columns and group of the state's rows. It does 4 operations for each 8 bytes, so it is
 // bound by reading and writing the state: 256 sequences, 16 heads of 128x128 (537
-// MB) take 111 us, 4.8 TB/s of a copy's 5.2; one sequence, 8 heads of 64 5 us, which
-// is a launch and three dependent passes.
+// MB) take 111 us, 4.8 TB/s of a copy's 5.2; one sequence, 8 heads of 64 4.5 us,
+// which is a launch and three dependent passes.
 template <typename T>
 __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per_row) {
   __shared__ float sq[256], sk[256], part[16][260];
