@@ -220,7 +220,9 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
  * width on; elements need only their own alignment, so that all may be parts
  * of one buffer). log_decay fp32 [H]: g, a constant of the model that no
  * gradient is taken of; -infinity is a head without memory, and g above 0 a
- * growing one. lengths int32 [B] on the device (NULL: all T; values are taken
+ * growing one: up to 2.5 its results are right as long as they and the states
+ * are in fp32's range, beyond, where the powers of 32 tokens leave it, some may
+ * be infinite or NaN instead (a single token's: beyond 88). lengths int32 [B] on the device (NULL: all T; values are taken
  * into [0, T]): tokens from a sequence's length on are neither read nor
  * written. States are fp32 [B][H][Dk][Dv], dense: s0 before the first token
  * (NULL: zeros), sT after the last (NULL: not wanted; may be s0 itself). Dk

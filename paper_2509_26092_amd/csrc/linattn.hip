@@ -12,6 +12,26 @@ namespace rn18 {
 
 namespace {
 
+// What a segment's tokens leave of a state (see Kept). Growth by more than exp(64)
+// goes in up to four steps: one factor would be infinite from exp(88.7) on, and make
+// NaN of a state of zeros. (exp(256) takes fp32's smallest number beyond its range.)
+struct KeptLong {
+  Kept step;
+  int steps;
+  __device__ inline float operator()(float x) const {
+    x = step(x);
+    for (int i = 1; i < steps; ++i) x = step(x);
+    return x;
+  }
+};
+__device__ inline KeptLong kept_long(int n, float g) {
+  const float t = (float)n * g;
+  if (!(t > 64.f)) return KeptLong{kept(n, g), 1};
+  const float most = t > 256.f ? 256.f : t;
+  const int steps = (int)ceilf(most / 64.f);
+  return KeptLong{kept(1, most / (float)steps), steps};
+}
+
 // Where a call has few heads, its sequences are cut into segments: a first
 // launch leaves what each segment (but the last) adds to the state, this one
 // turns these sums into the states that the segments start from, element by
@@ -24,7 +44,7 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p
   const int len = seq_len(c, b), m = e / c.N, n = e - m * c.N;
   const float g = c.log_decay[bh - b * c.H];
   float x = c.s_in ? c.s_in[(long)bh * per + (long)m * c.s_m + (long)n * c.s_n] : 0.f;
-  const Kept whole = kept(tokens, g);
+  const KeptLong whole = kept_long(tokens, g);
   float* at = c.states + (long)bh * p.nseg * per + (long)m * c.st_m + (long)n * c.st_n;
   for (int s = 0; s < p.nseg; s += U) {
     float add[U];
@@ -35,7 +55,7 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(Cores cs, Split p
       if (s + u >= p.nseg) break;
       at[(long)u * per] = x;
       const int k = min(max(len - (s + u) * tokens, 0), tokens);
-      if (k > 0) x = (k == tokens ? whole : kept(k, g))(x) + add[u];
+      if (k > 0) x = (k == tokens ? whole : kept_long(k, g))(x) + add[u];
     }
     at += (long)U * per;
   }
