@@ -706,7 +706,21 @@ int chunk_launch(const Cores& cs, const Split& p, hipStream_t s) {
   // segments, fp16 backward: 333 us, one contiguous range of blocks an XCD 450.)
   int mates = 1;
   for (int i = 0; i < cs.n; ++i) mates = std::max({mates, cs.c[i].q.group, cs.c[i].k.group});
-  auto heads = [&](int segs) { return (long)c.B * segs >= 64 ? c.H : mates; };
+  // Fewer of them where that leaves fewer than 64 units, which the XCDs share about
+  // evenly: all heads of one sequence over one key head would be one unit on one XCD,
+  // and seven of eight blocks of the grid empty. (us, with them all on one XCD and
+  // so, bf16 backward: 1x2048 tokens, 128 heads of 128 over one 1572 and 361, 1x4096,
+  // 64 of 256 over one 7527 and 1341, fp16 1x300, 32 of 128 over one 121 and 65; 8
+  // units in place of 64 are slower where a few more than 8 come out: bf16 2x2000, 32
+  // of 64 over 8 99 and 93.)
+  auto heads = [&](int segs) {
+    int h = (long)c.B * segs >= 64 ? c.H : mates;
+    for (int f = 2; h > 1 && (long)c.B * (c.H / h) * segs < 64;) {
+      if (h % f == 0) h /= f;
+      else f = f * f > h ? h : f + 1;
+    }
+    return h;
+  };
   auto grid = [&](int segs, int passes) {
     const int h = heads(segs);
     return dim3(ceil_div((long)c.B * (c.H / h) * segs, 8) * 8 * h * nb * passes);
