@@ -257,6 +257,8 @@ __global__ __launch_bounds__(256) void rms_fwd_short_kernel(RmsFwd a, Dropout d)
 // Rows beyond a block's registers: h is made and stored in one pass (where h
 // is x itself, nothing is stored) and read again for y, and once more for the
 // largest y where that is wanted. A thread reads what it has written itself.
+// The chunks' sums are added up in 64 bits: up to 2^20 of them are a thread's, and
+// in fp32 equal elements' roundings all go one way (1.4e-4 of y at 2^24 elements).
 template <typename T, bool DROP, bool Q8>
 __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a, Dropout d) {
   constexpr int VW = TT<T>::VW;
@@ -268,7 +270,8 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a, Dropout d)
   for (long r = blockIdx.x; r < a.R; r += gridDim.x, odd ^= 1) {
     const T *xr = (const T*)a.x + r * a.ldx, *rr = res ? (const T*)a.res + r * a.ldres : xr;
     T* hr = (T*)a.h + r * a.ldh;
-    float s = 0.f, t = 0.f, v[VW], gm[VW];
+    float t = 0.f, v[VW], gm[VW];
+    double s = 0.;
     uint4 qh;
     if (has_tail) {
       const T th = one_h<T, DROP>(xr[tail], rr[tail], res, key, r, tail);
@@ -279,10 +282,12 @@ __global__ __launch_bounds__(1024) void rms_fwd_long_kernel(RmsFwd a, Dropout d)
     for (int c = threadIdx.x; c < nch; c += 1024) {
       chunk_h<T, DROP>(v, load_chunk(xr + c * VW), load_chunk(rr + c * VW), res, key, r, c * VW, qh);
       if (a.h) store_chunk(hr + c * VW, qh);
+      float u = 0.f;
 #pragma unroll
-      for (int j = 0; j < VW; ++j) s += v[j] * v[j];
+      for (int j = 0; j < VW; ++j) u += v[j] * v[j];
+      s += u;
     }
-    const float rs = 1.0f / sqrtf(block_sum1024(s, sh) / (float)D + a.eps);
+    const float rs = 1.0f / sqrtf(block_sum1024((float)s, sh) / (float)D + a.eps);
     const T* src = a.h ? hr : xr;
     auto y_of = [&](int c) {
       unpack<T>(load_chunk(src + c * VW), v);
@@ -552,21 +557,24 @@ __global__ __launch_bounds__(1024) void rms_bwd_long_kernel(RmsBwd a, Dropout d)
     const T* drr = a.dr ? (const T*)a.dr + r * a.lddr : nullptr;
     T *dhr = a.dh ? (T*)a.dh + r * a.lddh : nullptr, *dxr = a.dx ? (T*)a.dx + r * a.lddx : nullptr;
     const float rs = a.rstd[r];
-    float s = 0.f, tg = 0.f, tx = 0.f;
+    float tg = 0.f, tx = 0.f;
+    double sum = 0.;   // (in 64 bits as in the forward pass)
     if (has_tail) {
       tg = TT<T>::to_f(dyr[tail]) * (a.gamma ? a.gamma[tail] : 1.f);
       tx = TT<T>::to_f(hr[tail]) * rs;
-      s = tg * tx;
+      sum = tg * tx;
     }
     float g[VW], v[VW], gm[VW];
     for (int c = threadIdx.x; c < nch; c += 1024) {
       unpack<T>(load_chunk(dyr + c * VW), g);
       unpack<T>(load_chunk(hr + c * VW), v);
       load_param<VW>(a.gamma, c * VW, 1.f, gm);
+      float u = 0.f;
 #pragma unroll
-      for (int j = 0; j < VW; ++j) s += g[j] * gm[j] * (v[j] * rs);
+      for (int j = 0; j < VW; ++j) u += g[j] * gm[j] * (v[j] * rs);
+      sum += u;
     }
-    s = block_sum1024(s, sh) / (float)D;
+    const float s = block_sum1024((float)sum, sh) / (float)D;
     if (has_tail) {
       const float w = rs * (tg - tx * s) + (drr ? TT<T>::to_f(drr[tail]) : 0.f);
       if (dhr) dhr[tail] = TT<T>::from_f(w);
@@ -590,15 +598,15 @@ __global__ __launch_bounds__(1024) void rms_bwd_long_kernel(RmsBwd a, Dropout d)
 }
 
 // Its parameter gradient: block (columns of 256, range of rows) writes one
-// partial row.
+// partial row, added up in 64 bits (the longest rows have one block to a column).
 template <typename T>
 __global__ __launch_bounds__(256) void rms_param_long_kernel(RmsBwd a, float* part, int Dp) {
   const long c = (long)blockIdx.x * 256 + threadIdx.x;
   if (c >= a.D) return;
-  float s = 0.f;
+  double s = 0.;
   for (long r = blockIdx.y; r < a.R; r += gridDim.y)
     s += TT<T>::to_f(((const T*)a.dy)[r * a.lddy + c]) * (TT<T>::to_f(((const T*)a.h)[r * a.ldh + c]) * a.rstd[r]);
-  part[(long)blockIdx.y * Dp + c] = s;
+  part[(long)blockIdx.y * Dp + c] = (float)s;
 }
 
 // ------------------------------------------------------------------ choice of kernel
