@@ -220,6 +220,8 @@ class TokenStudent:
     features, logits and parameters in fp32."""
 
     def __init__(self, classes, width=512, patch=16, dtype=torch.bfloat16, seed=0, blocks=0, heads=8, dropout=0.0):
+        if blocks < 0 or heads < 1:
+            raise ValueError("%d residual blocks of %d heads" % (blocks, heads))
         if dropout and not blocks:
             raise ValueError("dropout without residual blocks, whose branches it drops")
         g = torch.Generator(device="cuda").manual_seed(seed)
