@@ -137,8 +137,9 @@ int rn18op_dropout(int prec, const void* x, const void* res, void* y, int64_t R,
  * it as it is stored. res may be NULL (0), gamma fp32 [D] too (1), rstd fp32
  * [R] too (in inference); h may be NULL where it would be x itself (no res,
  * p = 0). h and y may each be x or res, but not the same. The sum of squares
- * is fp32's: beyond its range (elements from 1.8e19 on) rstd is 0; a row that
- * holds a NaN gives NaN, and one that holds an infinity NaN there and 0
+ * is fp32's: beyond its range (elements from 1.8e19 on) rstd is 0, and below it
+ * (for eps = 0 a row of elements below 1e-19 alone) inexact or infinite; a row
+ * that holds a NaN gives NaN, and one that holds an infinity NaN there and 0
  * elsewhere. */
 int rn18op_rmsnorm_fwd(int prec, const void* x, const void* res, const float* gamma, void* h, void* y, float* rstd,
                        int64_t R, int D, int64_t ldx, int64_t ldres, int64_t ldh, int64_t ldy, float eps, float p,
@@ -222,9 +223,9 @@ int rn18op_distill_loss(int prec, const void* z, const float* t_vals, const int3
  * gradient is taken of; -infinity is a head without memory, and g above 0 a
  * growing one: up to 2.5 its results are right as long as they and the states
  * are in fp32's range, beyond, where the powers of 32 tokens leave it, some may
- * be infinite or NaN instead (a single token's: beyond 88). lengths int32 [B] on the device (NULL: all T; values are taken
- * into [0, T]): tokens from a sequence's length on are neither read nor
- * written. States are fp32 [B][H][Dk][Dv], dense: s0 before the first token
+ * be infinite or NaN instead (a single token's: beyond 88). lengths int32 [B]
+ * on the device (NULL: all T; values are taken into [0, T]): tokens from a
+ * sequence's length on are neither read nor written. States are fp32 [B][H][Dk][Dv], dense: s0 before the first token
  * (NULL: zeros), sT after the last (NULL: not wanted; may be s0 itself). Dk
  * and Dv from 1 to 256, B T H up to 2^31 - 1, B H up to 2^20, T up to 2^26.
  * Sums and states are fp32; the products of 16-bit types keep the decayed and

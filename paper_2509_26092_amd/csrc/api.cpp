@@ -1845,7 +1845,7 @@ int rn18op_layernorm_bwd(int prec, const void* dy, const void* x, const float* g
   return RN18_OK;
 }
 
-// The dropout of (p, seed, step); *d is left alone for p = 0.
+// The dropout of (p, seed, step); for p = 0 all is kept, times 1.
 static int dropout_check(float p, uint64_t seed, uint64_t step, const uint64_t* step_add, Dropout* d) {
   if (!(p >= 0.f && p < 1.f)) return fail(RN18_EINVAL, "dropout rate must be in [0, 1)");
   if ((uintptr_t)step_add & 7u) return fail(RN18_EINVAL, "step_add is misaligned");

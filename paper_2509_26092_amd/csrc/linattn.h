@@ -95,11 +95,11 @@ __device__ inline int seq_len(const Core& c, int b) {
 // (the second terms of both with kv_scale). No power is above one for a decay
 // below one, and none infinite for a growth of up to exp(2.5) a token. (Beyond it
 // shorter chunks, or such heads token by token in a branch of their own, would do:
-// measured, 3 to 15% of every head's time in fp16, whose registers are full.) A wave takes 16 NT columns of a head's state through the chunks:
-// X stays in the accumulators of the matrix units, and so do the scores: what
-// comes out of one product, rows 4 (lane / 16) + 0..3 of each 16, is an operand
-// of the next whose inner index goes over these rows, if the other operand is
-// read in the same order. Only q, k and v pass through LDS, q and k once for
+// measured, 3 to 15% of every head's time in fp16, whose registers are full.) A wave
+// takes 16 NT columns of a head's state through the chunks: X stays in the
+// accumulators of the matrix units, and so do the scores: what comes out of one
+// product, rows 4 (lane / 16) + 0..3 of each 16, is an operand of the next whose
+// inner index goes over these rows, if the other operand is read in the same order. Only q, k and v pass through LDS, q and k once for
 // the W waves of a block, which share a head. The next chunk's rows are loaded
 // into registers meanwhile.
 //
@@ -114,10 +114,11 @@ __device__ inline int seq_len(const Core& c, int b) {
 // 5.2); 1x65537, 16 heads of 128, 340 us for 1.1 GB (the vector units are busy for
 // 48% of that, the matrix units for 31%) after 140 us for the segments' sums (561
 // MB, 4.0 TB/s); bf16 backward of the first, three passes, 140 us for 455 MB.
-// Slower or no faster: three waves of a SIMD (X leaves no room for them in the
-// registers), loads two chunks ahead (80 us and 67 for the first), rows in LDS 8 or
-// 12 banks further each, tables of the powers in LDS, a higher priority of waves
-// that load (434 and 436 us for all of the second).
+// Other ways are given below and there as a share of the same case's time in the
+// kernel of their day, measured side by side. Slower or no faster: three waves of a
+// SIMD (X leaves no room for them in the registers), loads two chunks ahead (19%
+// more for the first), rows in LDS 8 or 12 banks further each, tables of the powers
+// in LDS, a higher priority of waves that load (all equal).
 
 // A lane's operand of one step over KB of the inner index, in NP parts: places
 // 4 (lane / 16) + 0..3 of the first and of the second 16 in 16 bits, of 16 in
@@ -457,8 +458,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 
   // A chunk's results wait in registers for the next one's loads: stores are
   // counted with the loads behind them, and loads behind them would wait for
-  // stores that have only just begun (a chunk then waited for its stores: 78 us
-  // in place of 67 at 256x196 tokens, 8 heads of 64, bf16 forward).
+  // stores that have only just begun (a chunk then waited for its stores: 16% more
+  // at 256x196 tokens, 8 heads of 64, bf16 forward).
   uint4 result[CT][NT / 2][2];
   int results = 0;   // tokens of the chunk that waits
   auto flush = [&]() __attribute__((always_inline)) {
@@ -523,8 +524,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) out[it][nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
       }
-      // (one body for all of the inner index: 426 us in place of 434 with a branch
-      // in each step, 1x65537 tokens, 16 heads of 128, bf16 forward)
+      // (one body for all of the inner index: 2% less than with a branch in each step,
+      // 1x65537 tokens, 16 heads of 128, bf16 forward)
       auto products = [&](auto with_state) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < MP / KB; ++kb) {
@@ -666,8 +667,8 @@ __global__ __launch_bounds__(64 * W, (Tile<T, MP, NT, W>::WAVES)) void linattn_c
     }
   };
 
-  // (Two places in LDS and one barrier a chunk were no faster: 440 us at 1x65537, 16
-  // heads of 128, bf16 forward, 437 so; 80 and 71 at 256x196, 8 heads of 64.)
+  // (Two places in LDS and one barrier a chunk were no faster: equal at 1x65537, 16
+  // heads of 128, bf16 forward, 13% more at 256x196, 8 heads of 64.)
   if (total > 0) fetch(total);
   for (int left = total; left > 0; left -= C) {
     if (left < C) tails(left);
@@ -702,8 +703,9 @@ int chunk_launch(const Cores& cs, const Split& p, hipStream_t s) {
   const int nb = ceil_div(c.N, 16 * NT * W);
   // all heads of a token together where there are enough units to deal out so,
   // otherwise those that share keys and values. (256x196 tokens, 8 heads of 64,
-  // bf16 forward: 66 us, every head for itself 70; ragged sequences in 16
-  // segments, fp16 backward: 333 us, one contiguous range of blocks an XCD 450.)
+  // bf16 forward: 73 us, those that share keys alone 75, backward 139 and 142; ragged
+  // sequences in 22 segments, fp16 backward: one contiguous range of blocks an XCD 35%
+  // more.)
   int mates = 1;
   for (int i = 0; i < cs.n; ++i) mates = std::max({mates, cs.c[i].q.group, cs.c[i].k.group});
   // Fewer of them where that leaves fewer than 64 units, which the XCDs share about
@@ -736,10 +738,10 @@ int chunk_launch(const Cores& cs, const Split& p, hipStream_t s) {
   return launched();
 }
 
-// A wave takes 32 columns of the state: 64 were slower (83 us in place of 73 at
-// 256x196 tokens, 8 heads of 64, bf16, and 571 of 472 at 1x65537, 16 heads of
-// 128: too few waves beside the vector units' work on X), and 16 too (90, 658:
-// every wave computes the scores).
+// A wave takes 32 columns of the state: 64 were slower (14% at 256x196 tokens, 8
+// heads of 64, bf16 forward, and 21% at 1x65537, 16 heads of 128: too few waves
+// beside the vector units' work on X), and 16 too (23% and 39%: every wave computes
+// the scores).
 template <typename T, int WIDTHS>
 int widths_launch(const Cores& cs, int rows, int waves, const Split& p, hipStream_t s) {
   auto go = [&](auto r) {

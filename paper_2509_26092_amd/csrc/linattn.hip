@@ -72,7 +72,7 @@ struct GroupSum {
   int N[2];
 };
 // V columns a thread at a time, kGroupRun times in a block's run of columns.
-// (4: 266 us for that whole backward pass; 16, which are too few blocks, 287.)
+// (4: 273 us for that whole backward pass; 16, which are too few blocks, 290.)
 constexpr int kGroupRun = 4;
 template <typename T, int V>
 __global__ __launch_bounds__(256) void linattn_group_sum_kernel(GroupSum a, const int32_t* lengths, int B, int T_, int H,
@@ -173,25 +173,27 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinattnFwd a, int per
 }
 
 // Segments of a call: two waves for each SIMD, as many as fit there, where there
-// are few heads; up to 8192 tokens twice as many, which evens out sequences of
-// other lengths (6 ragged ones of up to 4095, 8 heads of 96, fp16 backward: 541
-// us, 592 without; but 1x65537, 16 heads of 128: 472 with twice as many, whose
-// states are then a sixth of the traffic, and 451 without). No segment is below
-// four chunks, and two are none: 1x1024, 8 heads of 64, bf16 forward takes 22 us
-// and 31 with eight chunks at least, 2x256 22 in two segments and 18 in one. The
-// same for a state and its transpose.
+// are few heads, and up to 8192 tokens twice as many, which evens out sequences of
+// other lengths (us; 6 ragged ones of up to 4095, 8 heads of 96, fp16 backward: 22
+// segments 264, 11 278, 6 301; but 1x65537, 16 heads of 128, bf16 forward: 32
+// segments 445, 64, whose states are a sixth of the traffic, 476, 16 495). No
+// segment but the last is below four chunks, and two are none: 1x1024, 8 heads of
+// 64, bf16 forward takes 23 in 8 segments of four, 31 in 4 and 55 whole, 2x256 22 in
+// two segments and 18 whole. The same for a state and its transpose.
 // No segments, whose sums are another pass over k and v, for heads that fill
 // the card by themselves, which a backward pass does sooner: its three passes
 // run side by side. us without segments and with them, where the rule begins,
-// backward: bf16 12x2048, 16 heads of 64 160 and 200, 11x1000, 8 heads of 128 134
-// and 176, fp32 12x1024, 16 of 128 634 and 764; below it bf16 16x3000, 8 of 64 228
-// and 196, fp32 (bound by the matrix units, which want more waves) 6x2048, 16 of
-// 128 814 and 728. Forward, sequences of up to 64 chunks: bf16 12x1024, 16 of 128
-// 88 and 135, 14x486 50 and 97; longer or fewer ones: 17x3000, 16 of 64 227 and
-// 134, 12x2048 106 and 99. A SIMD holds one wave of the widest states in place of
-// two, so that half as many heads of 129 columns or more fill the card: bf16
-// backward 4x1000, 8 of 256 170 and 321, forward 20x400, 4 of 256 78 and 139; half
-// of that forward, 4x1000, 165 and 128.
+// backward: bf16 12x2048, 16 heads of 64 159 and 202, 11x1000, 8 heads of 128 126
+// and 165, fp32 12x1024, 16 of 128 621 and 732; below it bf16 16x3000, 8 of 64 227
+// and 193, fp32 (bound by the matrix units, which want more waves) 6x2048, 16 of
+// 128 804 and 711. Just below it the count is past its best: bf16 21x3000, 8 of 64
+// 227 whole, 241 in 12 segments and 219 in 4, as is 16x3000 with 178 in 4. Forward,
+// sequences of up to 64 chunks: bf16 12x1024, 16 of 128 87 and 132, 14x486 50 and
+// 96, 12x2048 164 and 207; longer ones, below their rule: 17x3000, 16 of 64 226 and
+// 174. A SIMD holds one wave of the widest states in place of two, so that half as
+// many heads of 129 columns or more fill the card: bf16 backward 4x1000, 8 of 256
+// 164 and 302, forward 20x400, 4 of 256 75 and 130; half of that forward, 4x1000,
+// 162 and 72.
 Split split_of(int prec, int B, int T, int H, int M, int N, int passes) {
   const int all = std::max(1, ceil_div(T, kChunk)), beside = passes == 1 ? 1 : prec == PREC_F32 ? 2 : 3,
             widest = std::max(M, N) > 128 ? 2 : 1;
