@@ -245,7 +245,7 @@ int rn18op_linattn_fwd(int prec, const void* q, const void* k, const void* v, co
  *   S_t as above,  dq_t = scale S_t dO_t,
  *   G_t = exp(g) G_(t+1) + scale q_t dO_t^T,  exp(g) G_(length) = dS_T
  *   dk_t = G_t v_t,  dv_t = G_t^T k_t,  ds0 = exp(g) G_0
- * dk and dv are added up over the query heads that share a key head (in fp32).
+ * dk and dv are added up over the query heads that share a key head (in 64 bits).
  * ds0 may be NULL, or dS_T itself. */
 size_t rn18op_linattn_bwd_workspace(int prec, int B, int T, int H, int Hk, int Dk, int Dv);
 int rn18op_linattn_bwd(int prec, const void* q, const void* k, const void* v, const void* dout,

@@ -56,3 +56,24 @@ def test_all_heads_over_one_key_head():
     assert torch.equal(dq, (dots * k.double()).to(torch.bfloat16))
     assert torch.equal(dk, (dots * q.double()).sum(0, keepdim=True).to(torch.bfloat16))
     assert torch.equal(dv, (sums * k.double()).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("G", [4096, 1 << 17])
+@pytest.mark.parametrize("q,do", [(1.1, 0.83), (0.7, 1.3)])
+@pytest.mark.parametrize("D", [8, 5])
+def test_equal_gradients_of_many_heads(G, q, do, D):
+    """Heads that share a key head and give it equal gradients, whose roundings
+    all go the same way: dk = G q (dO . v), dv = G dO (q . k), of terms of one
+    sign. fp32: a term is off by (2 D + 4) 2^-24 at most, the sum by 2^-23."""
+    import torch
+    full = lambda *s: torch.full(s[:-1], float(s[-1]), device="cuda")
+    sizes = (1, 1, G, 1, D, D)
+    qd, kd, vd, dod = full(G, D, q), full(1, D, 0.9), full(1, D, 1.7), full(G, D, do)
+    dq, dk, dv = torch.empty_like(qd), torch.empty_like(kd), torch.empty_like(vd)
+    ws = ws_of(B.rn18op_linattn_bwd_workspace(PREC["fp32"], *sizes))
+    B.rn18op_linattn_bwd(PREC["fp32"], qd, kd, vd, dod, torch.zeros(G, device="cuda"), None, None, None, dq, dk, dv, None,
+                         *sizes, G * D, D, D, G * D, G * D, D, D, 1.0, ws)
+    first = lambda t: t.double().flatten()[0].item()
+    a, b, k, v = first(qd), first(dod), first(kd), first(vd)
+    for got, ref in ((dk, G * a * D * b * v), (dv, G * b * D * a * k)):
+        assert (got.double() - ref).abs().max().item() <= (2 * D + 6) * 2.0 ** -24 * ref
